@@ -385,10 +385,134 @@ mca_status mca_run_channels(mca_handle* h, uint64_t n_trials, uint64_t seed, int
  * otherwise. */
 mca_status mca_selftest_wait_timeout(int32_t* status, double* waited_ms);
 
+/* ---------------------------------------------------------------------------------------------
+ * A trained net's answers: layers in 8-bit integers, log probabilities of given symbols, and the same
+ * from a handle (mca_predict, mca_score). The calls without a handle share these rules:
+ *  - Arrays are DEVICE arrays of the current device; `stream` (a cudaStream_t, NULL = the legacy
+ *    default stream) belongs to it. Work is queued there and the call returns without waiting; nothing
+ *    is allocated, and the calls may be captured into a graph. They keep no state: calls may run at the
+ *    same time on several streams or threads, each with its own outputs and workspace.
+ *  - Matrices are row-major with unit column stride; ld is the distance between rows in elements (at
+ *    least the row's length; not looked at for a single row). Elements lie on their natural alignment;
+ *    rows that start on 16-byte boundaries are read faster. Nothing outside the rows' elements is
+ *    written. Outputs overlap no input, except where it is said.
+ *  - rows = 0 is a call without work. Errors: INVALID (also for host pointers or pointers of another
+ *    device), OOM (workspace too small), CUDA; the message is that of mca_last_error(NULL).
+ * ------------------------------------------------------------------------------------------- */
+
+/* Element type of a caller's matrix. */
+typedef enum { MCA_DTYPE_FP32 = 0, MCA_DTYPE_FP16 = 1, MCA_DTYPE_BF16 = 2 } mca_dtype;
+
+/* Rows in 8 bits: scale[r] = fp32(max_c |x[r, c]| / 127), codes[r, c] = x[r, c] / scale[r] rounded to
+ * the nearest integer (halves to the even one; the quotient is not rounded before), at most 127 in magnitude, so
+ * that x ~ scale * code. A row of zeros, or one whose scale is less than fp32 can hold, has scale 0 and
+ * codes 0; a row with a NaN or an infinity has scale NaN and codes 0. x: [rows x cols] of `dtype`;
+ * codes: [rows x cols]; scale: [rows]. cols >= 1. */
+mca_status mca_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx,
+                             int8_t* codes, int64_t ldc, float* scale, void* stream);
+
+/* A layer on codes: y[r, n] = act(float(s) * x_scale[r] * w_scale[n] + bias[n]) with the integer sum s =
+ * sum_k x[r, k] * w[n, k], which is exact; the products and the sum after it round to fp32, from left to right,
+ * and y to `dtype` (to an infinity beyond fp16's range). */
+typedef struct {
+  int64_t rows;            /* samples or tokens */
+  int32_t n_in, n_out;     /* 1 <= n_in <= 131071: sums of any codes stay below 2^31 */
+  const int8_t* x;         /* [rows x n_in] */
+  int64_t ldx;
+  const float* x_scale;    /* [rows] */
+  const int8_t* w;         /* [n_out x n_in] */
+  int64_t ldw;
+  const float* w_scale;    /* [n_out] */
+  const float* bias;       /* [n_out], nullable */
+  void* y;                 /* [rows x n_out] of `dtype` */
+  int64_t ldy;
+  int32_t dtype;           /* mca_dtype of y */
+  int32_t act;             /* mca_act */
+  float act_param;         /* gamma of MCA_ACT_GAUSSIAN; ignored otherwise */
+  void* workspace;         /* 256-byte aligned, mca_code_linear_workspace_size() bytes, for this call's
+                              duration; NULL where that is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} mca_code_linear_args;
+
+/* Bytes of workspace that mca_code_linear needs for these sizes, pointers and strides: aligned copies of
+ * operands whose rows do not start on 16-byte boundaries (0 where both do). Host only. */
+mca_status mca_code_linear_workspace_size(const mca_code_linear_args* a, size_t* bytes);
+mca_status mca_code_linear(const mca_code_linear_args* a);
+
+/* Log probabilities (natural log) of given symbols under softmax(logits[r, :]), the entropy of that
+ * distribution and the most probable symbols, in one pass over the logits. A logit of -inf takes its
+ * symbol out. Sums are held in fp32. Special rows:
+ *  - targets[r] = -1: no symbol is asked for, logprob[r] = 0. Any other target outside [0, vocab):
+ *    logprob[r] = NaN.
+ *  - every logit -inf: lse = -inf, logprob = -inf, entropy = 0, no alternatives.
+ *  - a NaN or +inf among the logits: lse, entropy, logprob (of a target >= 0) and top_logprob are NaN,
+ *    top_index -1. */
+typedef struct {
+  const void* logits;      /* [rows x vocab] of `dtype` */
+  int32_t dtype;           /* mca_dtype */
+  int32_t vocab;           /* >= 1 */
+  int64_t rows, ld;
+  const int32_t* targets;  /* [rows]; nullable where logprob is */
+  float* logprob;          /* [rows], nullable: logits[r, targets[r]] - lse[r] */
+  float* entropy;          /* [rows], nullable: -sum p ln p, in nats */
+  float* lse;              /* [rows], nullable: ln sum exp(logits[r, :]) */
+  int32_t top;             /* alternatives per row, 0..32 */
+  float* top_logprob;      /* [rows x top]: the largest log probabilities in falling order, equal logits
+                              in the order of their index; -inf behind the last symbol */
+  int32_t* top_index;      /* [rows x top]: their symbols; -1 behind the last one */
+  void* stream;
+} mca_token_logprobs_args;
+mca_status mca_token_logprobs(const mca_token_logprobs_args* a);
+
+/* The gradient of g_logprob[r] * logprob[r] + g_entropy[r] * entropy[r], summed over rows, with respect to
+ * the logits: grad[r, v] = g_logprob ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy), with p_v = exp(logits[r, v] - lse[r]) from the
+ * forward call's lse and entropy. Rows without a target (-1) take no part of g_logprob, with another target
+ * outside [0, vocab) their gradient is NaN; rows whose logits are all -inf have gradient 0. A nullable array that is NULL counts as zeros (g_entropy and entropy go together, g_logprob and
+ * targets too; not both pairs NULL). grad: [rows x vocab] of `dtype`; it may be `logits` itself with the same
+ * ld, and overlaps it in no other way. */
+typedef struct {
+  const void* logits;
+  int32_t dtype;
+  int32_t vocab;
+  int64_t rows, ld;
+  const int32_t* targets;  /* [rows], nullable */
+  const float* lse;        /* [rows] */
+  const float* entropy;    /* [rows], nullable */
+  const float* g_logprob;  /* [rows], nullable */
+  const float* g_entropy;  /* [rows], nullable */
+  void* grad;
+  int64_t ldg;
+  void* stream;
+} mca_token_logprobs_backward_args;
+mca_status mca_token_logprobs_backward(const mca_token_logprobs_backward_args* a);
+
+/* What the net of handle h says about its own samples, from the cached fields: the logits of every sample
+ * (MLP, softmax_ce: the last layer's activations) or predicted position (Transformer: sequence by sequence),
+ * and mca_token_logprobs of the labels / next tokens under them. rows = N or n_seq * ctx, classes = n_out of the
+ * last layer or vocab. logits: [rows x classes] fp32; the others as in mca_token_logprobs, nullable
+ * (top_logprob and top_index where top = 0). DEVICE arrays of the handle's device. Queued on the handle's
+ * stream, without waiting; the state does not change. -sum(logprob) / rows is mca_loss up to rounding.
+ * Errors: INVALID, UNSUPPORTED (loss mse_onehot), CUDA. */
+mca_status mca_score(mca_handle* h, float* logits, int32_t top, float* logprob, float* entropy,
+                     float* lse, float* top_logprob, int32_t* top_index);
+
+/* Answers of an MLP handle's net, with its present weights, to n new samples in 8-bit integers: every layer
+ * quantises its inputs per sample (mca_quantize_rows) and multiplies them with weights in 8 bits per
+ * output neuron (mca_code_linear; a ternary layer's codes with its scale, other layers' effective weights
+ * quantised by row). x: [n x n_in of the first layer] fp32, row stride ldx; out: [n x n_out of the last layer] fp32,
+ * its activations, contiguous. Hidden activations are held in fp16 (transfer functions bounded by 1) or fp32. workspace:
+ * mca_predict_workspace_size() bytes, 256-byte aligned. DEVICE arrays of the handle's device. Queued
+ * on the handle's stream, without waiting. Errors: INVALID, UNSUPPORTED (a Transformer handle), OOM (workspace
+ * too small), CUDA. */
+mca_status mca_predict_workspace_size(mca_handle* h, int64_t n, size_t* bytes);
+mca_status mca_predict(mca_handle* h, const float* x, int64_t n, int64_t ldx, float* out,
+                       void* workspace, size_t workspace_bytes);
+
 void mca_destroy(mca_handle* h);
 
-/* Message of the last failed call on h (h may be NULL: then the last failed mca_create or
- * mca_workspace_size of this thread). Never NULL. */
+/* Message of the last failed call on h (h may be NULL: then the last failed mca_create,
+ * mca_workspace_size or other call without a handle of this thread). Never NULL. */
 const char* mca_last_error(mca_handle* h);
 
 #ifdef __cplusplus

@@ -1052,6 +1052,8 @@ mca_status run_tfm_pipelined(mca_handle* h, mca::TfmArgs ta, uint64_t n_trials) 
 
 namespace mca {
 Mlp2Args handle_mlp2_args(mca_handle* h) { return mlp2_args(h); }
+TfmArgs handle_tfm_args(mca_handle* h) { return tfm_args(h); }
+mca_status fail_message(mca_handle* h, mca_status st, const char* msg) { return fail(h, st, "%s", msg); }
 }  // namespace mca
 
 extern "C" {

@@ -432,6 +432,9 @@ struct mca_handle;
 namespace mca {
 // Kernel arguments of a handle's trial loop (its state and workspace scratch).
 Mlp2Args handle_mlp2_args(mca_handle* h);
+TfmArgs handle_tfm_args(mca_handle* h);
+// st, with the message that mca_last_error(h) then returns.
+mca_status fail_message(mca_handle* h, mca_status st, const char* msg);
 
 }  // namespace mca
 

@@ -10,7 +10,8 @@ import ctypes
 import os
 from ctypes import (POINTER, Structure, c_char_p, c_double, c_float, c_int8, c_int32, c_int64,
                     c_size_t, c_uint8, c_uint32, c_uint64, c_void_p)
-from typing import Optional, Sequence
+from contextlib import contextmanager
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -23,6 +24,8 @@ ACT = {"identity": 0, "tanh": 1, "sigmoid": 2, "relu": 3, "gaussian": 4, "gelu":
 LOSS = {"mse_onehot": 0, "softmax_ce": 1}
 WKIND = {"fp32": 0, "ternary_i8": 1, "masked_fp32": 2}
 OP = {"replace": 0, "perturb": 1}
+DTYPE = {"float32": 0, "float16": 1, "bfloat16": 2}
+MAX_TOP = 32
 
 
 class mca_layer(Structure):
@@ -71,6 +74,28 @@ class mca_trace_rec(Structure):
                 ("S", c_double)]
 
 
+class mca_code_linear_args(Structure):
+    _fields_ = [("rows", c_int64), ("n_in", c_int32), ("n_out", c_int32), ("x", c_void_p),
+                ("ldx", c_int64), ("x_scale", c_void_p), ("w", c_void_p), ("ldw", c_int64),
+                ("w_scale", c_void_p), ("bias", c_void_p), ("y", c_void_p), ("ldy", c_int64),
+                ("dtype", c_int32), ("act", c_int32), ("act_param", c_float),
+                ("workspace", c_void_p), ("workspace_bytes", c_size_t), ("stream", c_void_p)]
+
+
+class mca_token_logprobs_args(Structure):
+    _fields_ = [("logits", c_void_p), ("dtype", c_int32), ("vocab", c_int32), ("rows", c_int64),
+                ("ld", c_int64), ("targets", c_void_p), ("logprob", c_void_p),
+                ("entropy", c_void_p), ("lse", c_void_p), ("top", c_int32),
+                ("top_logprob", c_void_p), ("top_index", c_void_p), ("stream", c_void_p)]
+
+
+class mca_token_logprobs_backward_args(Structure):
+    _fields_ = [("logits", c_void_p), ("dtype", c_int32), ("vocab", c_int32), ("rows", c_int64),
+                ("ld", c_int64), ("targets", c_void_p), ("lse", c_void_p), ("entropy", c_void_p),
+                ("g_logprob", c_void_p), ("g_entropy", c_void_p), ("grad", c_void_p),
+                ("ldg", c_int64), ("stream", c_void_p)]
+
+
 TRACE_DTYPE = np.dtype([("tau", np.uint64), ("idx", np.uint32), ("accept", np.int32),
                         ("old_w", np.float32), ("new_w", np.float32), ("valid", np.int32),
                         ("forced", np.int32), ("dS", np.float64), ("S", np.float64)])
@@ -104,6 +129,17 @@ SIGNATURES = {
                                    c_int64, POINTER(c_int32)]),
     "mca_run_channels": (c_int32, [c_void_p, c_uint64, c_uint64, c_int32, c_void_p, c_void_p]),
     "mca_selftest_wait_timeout": (c_int32, [POINTER(c_int32), POINTER(c_double)]),
+    "mca_quantize_rows": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p,
+                                    c_int64, c_void_p, c_void_p]),
+    "mca_code_linear_workspace_size": (c_int32, [POINTER(mca_code_linear_args),
+                                                 POINTER(c_size_t)]),
+    "mca_code_linear": (c_int32, [POINTER(mca_code_linear_args)]),
+    "mca_token_logprobs": (c_int32, [POINTER(mca_token_logprobs_args)]),
+    "mca_token_logprobs_backward": (c_int32, [POINTER(mca_token_logprobs_backward_args)]),
+    "mca_score": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                            c_void_p]),
+    "mca_predict_workspace_size": (c_int32, [c_void_p, c_int64, POINTER(c_size_t)]),
+    "mca_predict": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_size_t]),
     "mca_destroy": (None, [c_void_p]),
     "mca_last_error": (c_char_p, [c_void_p]),
 }
@@ -169,9 +205,12 @@ def _domain(d) -> mca_domain:
 class Handle:
     """Owns one mca_handle plus the torch tensors the library borrows (workspace, dataset)."""
 
-    def __init__(self, ptr, keep):
+    def __init__(self, ptr, keep, stream=0, rows=0, classes=0, n_in=0):
         self.ptr = ptr
         self._keep = keep
+        self.stream = stream or 0        # cudaStream_t of the handle's work
+        self.rows, self.classes = rows, classes     # samples or predicted positions, and their classes
+        self.n_in = n_in                 # MLP: input features
 
     def close(self):
         if self.ptr:
@@ -222,7 +261,7 @@ def mca_create(layers, loss: str, domain, X, y, init, K: int = 32, resync_period
     h = c_void_p(None)
     _check(lib.mca_create(L, len(layers), LOSS[loss], ctypes.byref(dom), ctypes.byref(ds),
                           _ptr(init), ctypes.byref(opt), ctypes.byref(h)))
-    return Handle(h, keep)
+    return Handle(h, keep, stream, int(X.shape[0]), int(layers[-1].n_out), int(layers[0].n_in))
 
 
 def _tfm_spec(sp) -> mca_tfm_spec:
@@ -257,7 +296,7 @@ def mca_create_transformer(spec, domain, tokens, init, K: int = 32, resync_perio
     h = c_void_p(None)
     _check(lib.mca_create_transformer(ctypes.byref(sp), ctypes.byref(dom), _ptr(tokens), n_seq,
                                       _ptr(init), ctypes.byref(opt), ctypes.byref(h)))
-    return Handle(h, [tokens, init, ws])
+    return Handle(h, [tokens, init, ws], stream, n_seq * int(spec.ctx), int(spec.vocab))
 
 
 def create_from_tfm_workload(wl, device: bool = True, **kw) -> Handle:
@@ -379,6 +418,302 @@ def mca_selftest_wait_timeout():
     st, ms = ctypes.c_int32(-1), ctypes.c_double(0.0)
     _check(load_library().mca_selftest_wait_timeout(ctypes.byref(st), ctypes.byref(ms)))
     return st.value, ms.value
+
+
+# ------------------------------------------------------------------------------------------------
+# A trained net's answers. Tensors are CUDA tensors of one device, matrices with unit column stride;
+# results are new tensors (or the ones given). Work is queued on `stream` (a cudaStream_t, default:
+# the device's current torch stream), and tensors made here belong to it.
+# ------------------------------------------------------------------------------------------------
+
+def _cuda(name, t, dtypes, device=None, ndim=1):
+    """Checks a tensor argument."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: not a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    if t.dim() != ndim:
+        raise ValueError(f"{name}: {t.dim()} dimensions, expected {ndim}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: stride {t.stride(-1)} between elements of a row, expected 1")
+
+
+def _vector(name, t, n, dtype, device):
+    """Address of a vector argument of n elements (None: NULL)."""
+    if t is None:
+        return None
+    _cuda(name, t, (dtype,), device)
+    if t.shape[0] != n:
+        raise ValueError(f"{name}: {t.shape[0]} elements, expected {n}")
+    return t.data_ptr()
+
+
+def _ld(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _float_types():
+    import torch
+    return torch.float32, torch.float16, torch.bfloat16
+
+
+def _dtype_code(dtype) -> int:
+    try:
+        return DTYPE[str(dtype).split(".")[-1]]
+    except KeyError:
+        raise ValueError(f"dtype {dtype}: expected float32, float16 or bfloat16") from None
+
+
+@contextmanager
+def _other(device, stream):
+    """The device and stream that are not the current ones, for allocations and launches."""
+    import torch
+    with torch.cuda.device(device):
+        if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
+            yield
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if stream
+                                   else torch.cuda.default_stream(device)):
+                yield
+
+
+def _on(device, stream, call):
+    """call(stream's cudaStream_t) with the device current and tensors allocated on the stream."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        cur = torch.cuda.current_stream().cuda_stream
+        if stream is None or stream == cur:
+            return call(cur)
+    with _other(device, stream):
+        return call(torch.cuda.current_stream().cuda_stream)
+
+
+def mca_quantize_rows(x, codes=None, scale=None, stream=None):
+    """Rows of x [rows, cols] in 8 bits: (codes [rows, cols] int8, scale [rows] float32), x ~ scale *
+    codes. New codes' rows start on 16-byte boundaries (a view of a wider matrix when cols is not a
+    multiple of 16)."""
+    import torch
+    _cuda("x", x, _float_types(), ndim=2)
+    rows, cols = x.shape
+    dev = x.device
+    if codes is not None:
+        _cuda("codes", codes, (torch.int8,), dev, 2)
+        if codes.shape != x.shape:
+            raise ValueError(f"codes: shape {tuple(codes.shape)}, expected {tuple(x.shape)}")
+    _vector("scale", scale, rows, torch.float32, dev)
+
+    def call(s):
+        c = codes if codes is not None else torch.empty(
+            (rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=dev)[:, :cols]
+        sc = scale if scale is not None else torch.empty(rows, dtype=torch.float32, device=dev)
+        _check(load_library().mca_quantize_rows(x.data_ptr(), _dtype_code(x.dtype), rows, cols,
+                                                _ld(x), c.data_ptr(), _ld(c), sc.data_ptr(), s))
+        return c, sc
+
+    return _on(dev, stream, call)
+
+
+def _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype):
+    import torch
+    _cuda("x_codes", x_codes, (torch.int8,), ndim=2)
+    dev = x_codes.device
+    _cuda("w_codes", w_codes, (torch.int8,), dev, 2)
+    rows, n_in = x_codes.shape
+    n_out = w_codes.shape[0]
+    if w_codes.shape[1] != n_in:
+        raise ValueError(f"w_codes: {w_codes.shape[1]} columns, x_codes has {n_in}")
+    return mca_code_linear_args(
+        rows, n_in, n_out, x_codes.data_ptr(), _ld(x_codes),
+        _vector("x_scale", x_scale, rows, torch.float32, dev), w_codes.data_ptr(), _ld(w_codes),
+        _vector("w_scale", w_scale, n_out, torch.float32, dev),
+        _vector("bias", bias, n_out, torch.float32, dev), None, n_out,
+        0 if dtype is None else _dtype_code(dtype), ACT[act], float(act_param), None, 0, None)
+
+
+def mca_code_linear_workspace_size(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity",
+                                   act_param: float = 0.0, dtype=None) -> int:
+    """Bytes of workspace of mca_code_linear (0 where the rows of both operands start on 16-byte
+    boundaries)."""
+    a = _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype)
+    n = c_size_t(0)
+    _check(load_library().mca_code_linear_workspace_size(ctypes.byref(a), ctypes.byref(n)))
+    return n.value
+
+
+def mca_code_linear(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity",
+                    act_param: float = 0.0, dtype=None, out=None, workspace=None, stream=None):
+    """act((x_codes w_codes^T) * x_scale[:, None] * w_scale + bias), sums exact: [rows, n_out] of
+    `dtype` (default: out's, or float32). workspace: a uint8 CUDA tensor of at least
+    mca_code_linear_workspace_size bytes on a 256-byte boundary (default: allocated for the call)."""
+    import torch
+    if out is not None:
+        _cuda("out", out, _float_types(), x_codes.device, 2)
+        if dtype is not None and dtype != out.dtype:
+            raise ValueError(f"out: dtype {out.dtype}, expected {dtype}")
+        dtype = out.dtype
+    a = _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype)
+    dev = x_codes.device
+    if out is not None and tuple(out.shape) != (a.rows, a.n_out):
+        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(a.rows, a.n_out)}")
+    if workspace is not None:
+        _cuda("workspace", workspace, (torch.uint8,), dev)
+    lib = load_library()
+
+    def call(s):
+        y = out if out is not None else torch.empty((a.rows, a.n_out),
+                                                    dtype=dtype or torch.float32, device=dev)
+        ws = workspace
+        if ws is None:
+            n = c_size_t(0)
+            _check(lib.mca_code_linear_workspace_size(ctypes.byref(a), ctypes.byref(n)))
+            if n.value:
+                ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        if ws is not None and ws.numel():
+            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        a.y, a.ldy, a.stream = y.data_ptr(), _ld(y), s
+        _check(lib.mca_code_linear(ctypes.byref(a)))
+        return y
+
+    return _on(dev, stream, call)
+
+
+class TokenLogprobs(NamedTuple):
+    """Of every row of logits; None for what was not asked for."""
+    logprob: object          # [rows] float32, of the target
+    entropy: object          # [rows] float32
+    lse: object              # [rows] float32
+    top_logprob: object      # [rows, top] float32
+    top_index: object        # [rows, top] int32
+
+
+def _logprob_outputs(rows, top, targets, dev):
+    import torch
+
+    def new(*shape):
+        return torch.empty(shape, dtype=torch.float32, device=dev)
+    return TokenLogprobs(new(rows) if targets else None, new(rows), new(rows),
+                         new(rows, top) if top else None,
+                         torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def mca_token_logprobs(logits, targets=None, top: int = 0, stream=None) -> TokenLogprobs:
+    """Log probabilities of targets [rows] (int32, -1: none) under softmax of each row of logits [rows,
+    vocab], entropies, log-sum-exps and the `top` most probable symbols (at most 32)."""
+    import torch
+    _cuda("logits", logits, _float_types(), ndim=2)
+    rows, vocab = logits.shape
+    dev = logits.device
+    t = _vector("targets", targets, rows, torch.int32, dev)
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError(f"top = {top} outside 0..{MAX_TOP}")
+
+    def call(s):
+        r = _logprob_outputs(rows, top, targets is not None, dev)
+        a = mca_token_logprobs_args(
+            logits.data_ptr(), _dtype_code(logits.dtype), vocab, rows, _ld(logits), t,
+            _addr(r.logprob), r.entropy.data_ptr(), r.lse.data_ptr(), top, _addr(r.top_logprob),
+            _addr(r.top_index), s)
+        _check(load_library().mca_token_logprobs(ctypes.byref(a)))
+        return r
+
+    return _on(dev, stream, call)
+
+
+def mca_token_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy=None, out=None,
+                                stream=None):
+    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits, from the
+    lse and entropy of mca_token_logprobs. g_logprob (with targets) or g_entropy (with entropy) may be
+    None. out: [rows, vocab] of the logits' dtype, which may be `logits` itself."""
+    import torch
+    _cuda("logits", logits, _float_types(), ndim=2)
+    rows, vocab = logits.shape
+    dev = logits.device
+    f32 = torch.float32
+    v = [_vector("targets", targets, rows, torch.int32, dev),
+         _vector("lse", lse, rows, f32, dev), _vector("entropy", entropy, rows, f32, dev),
+         _vector("g_logprob", g_logprob, rows, f32, dev),
+         _vector("g_entropy", g_entropy, rows, f32, dev)]
+    if out is not None:
+        _cuda("out", out, (logits.dtype,), dev, 2)
+        if out.shape != logits.shape:
+            raise ValueError(f"out: shape {tuple(out.shape)}, expected {tuple(logits.shape)}")
+
+    def call(s):
+        g = out if out is not None else torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
+        a = mca_token_logprobs_backward_args(logits.data_ptr(), _dtype_code(logits.dtype), vocab,
+                                             rows, _ld(logits), *v, g.data_ptr(), _ld(g), s)
+        _check(load_library().mca_token_logprobs_backward(ctypes.byref(a)))
+        return g
+
+    return _on(dev, stream, call)
+
+
+@contextmanager
+def _handle_stream(h: Handle, *inputs):
+    """The handle's stream as the current one: its work follows what is queued on the caller's stream
+    (which made the inputs), and the caller's stream goes on after it."""
+    import torch
+    cur = torch.cuda.current_stream()
+    if cur.cuda_stream == h.stream:
+        yield []
+        return
+    st = torch.cuda.ExternalStream(h.stream) if h.stream else torch.cuda.default_stream()
+    st.wait_stream(cur)
+    made = []
+    with torch.cuda.stream(st):
+        yield made
+    for t in inputs:
+        t.record_stream(st)
+    cur.wait_stream(st)
+    for t in made:
+        t.record_stream(cur)
+
+
+def mca_score(h: Handle, top: int = 0):
+    """(logits [rows, classes], TokenLogprobs of the labels / next tokens) of the handle's own samples
+    under its present weights."""
+    import torch
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError(f"top = {top} outside 0..{MAX_TOP}")
+    with _handle_stream(h) as made:
+        logits = torch.empty((h.rows, h.classes), dtype=torch.float32, device="cuda")
+        r = _logprob_outputs(h.rows, top, True, "cuda")
+        _check(load_library().mca_score(h.ptr, logits.data_ptr(), top, _addr(r.logprob),
+                                        _addr(r.entropy), _addr(r.lse), _addr(r.top_logprob),
+                                        _addr(r.top_index)), h.ptr)
+        made += [logits] + [t for t in r if t is not None]
+    return logits, r
+
+
+def mca_predict_workspace_size(h: Handle, n: int) -> int:
+    b = c_size_t(0)
+    _check(load_library().mca_predict_workspace_size(h.ptr, n, ctypes.byref(b)), h.ptr)
+    return b.value
+
+
+def mca_predict(h: Handle, x):
+    """Activations [n, n_out] float32 of an MLP handle's last layer for new samples x [n, n_in]
+    (float32), every layer in 8-bit integers."""
+    import torch
+    _cuda("x", x, (torch.float32,), ndim=2)
+    if h.n_in and x.shape[1] != h.n_in:
+        raise ValueError(f"x: {x.shape[1]} columns, the net has {h.n_in} inputs")
+    n = x.shape[0]
+    with _handle_stream(h, x) as made:
+        nbytes = mca_predict_workspace_size(h, n)
+        out = torch.empty((n, h.classes), dtype=torch.float32, device="cuda")
+        ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        _check(load_library().mca_predict(h.ptr, x.data_ptr(), n, _ld(x), out.data_ptr(),
+                                          ws.data_ptr() if nbytes else None, nbytes), h.ptr)
+        made.append(out)
+    return out
 
 
 def mca_destroy(h: Handle):
