@@ -435,8 +435,9 @@ typedef struct {
   void* stream;
 } mca_code_linear_args;
 
-/* Bytes of workspace that mca_code_linear needs for these sizes, pointers and strides: aligned copies of
- * operands whose rows do not start on 16-byte boundaries (0 where both do). Host only. */
+/* Bytes of workspace that mca_code_linear needs for these sizes, pointers and strides (it may be 0): for many
+ * samples the codes of both operands as fp16, for few aligned copies of operands whose rows do not start on
+ * 16-byte boundaries. Host only. */
 mca_status mca_code_linear_workspace_size(const mca_code_linear_args* a, size_t* bytes);
 mca_status mca_code_linear(const mca_code_linear_args* a);
 

@@ -224,7 +224,7 @@ constexpr int64_t kPredictElems = 32 << 20;
 
 struct PredictPlan {
   int64_t chunk, width;           // samples per pass; the widest layer input or output
-  size_t codes, scale, hidden, w, w_scale, total;   // offsets
+  size_t codes, scale, hidden, w, w_scale, product, total;   // offsets
 };
 
 PredictPlan predict_plan(const mca_handle* h, int64_t n) {
@@ -248,6 +248,16 @@ PredictPlan predict_plan(const mca_handle* h, int64_t n) {
   p.hidden = take(4 * e);
   p.w = take(wb);
   p.w_scale = take(4 * outs);
+  size_t product = 0;
+  for (const mca_layer& L : h->layers) {
+    mca_code_linear_args a{};
+    a.rows = p.chunk;
+    a.n_in = L.n_in;
+    a.n_out = L.n_out;
+    a.ldx = a.ldw = round16(L.n_in);
+    product = std::max(product, mca::code_linear_workspace(a));
+  }
+  p.product = take(product);
   p.total = at;
   return p;
 }
@@ -457,6 +467,7 @@ mca_status mca_predict(mca_handle* h, const float* x, int64_t n, int64_t ldx, fl
       a.dtype = !last && bounded_by_one(L) ? MCA_DTYPE_FP16 : MCA_DTYPE_FP32;
       a.act = L.act;
       a.act_param = L.act_param;
+      a.workspace = ws + p.product;
       e = mca::launch_quantize_rows(in, in_dtype, m, L.n_in, in_ld, codes, a.ldx, scale, h->stream);
       if (e == cudaSuccess) e = mca::launch_code_linear(a, h->stream);
       h->launches += 2;

@@ -6,12 +6,12 @@ namespace mca {
 
 namespace {
 
+constexpr int64_t kPairRows = 128;
+
+bool use_pair(const mca_code_linear_args& a) { return a.rows > kPairRows; }
+
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
-
-bool aligned(const int8_t* p, int64_t rows, int64_t ld) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || ld % 16 == 0);
-}
 
 // Sixteen codes per thread, behind the last column zeros.
 __global__ void __launch_bounds__(256) align_rows_kernel(const int8_t* __restrict__ src, int64_t rows,
@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const int8_t* __restric
 }
 
 cudaError_t align_rows(const int8_t** p, int64_t rows, int cols, int64_t* ld, char** ws, cudaStream_t s) {
-  if (aligned(*p, rows, *ld)) return cudaSuccess;
+  if (code_rows_aligned(*p, rows, *ld)) return cudaSuccess;
   int8_t* dst = reinterpret_cast<int8_t*>(*ws);
   const int units = (cols + 15) / 16;
   align_rows_kernel<<<(unsigned int)((rows * units + 255) / 256), 256, 0, s>>>(*p, rows, cols, *ld, dst,
@@ -46,13 +46,15 @@ cudaError_t align_rows(const int8_t** p, int64_t rows, int cols, int64_t* ld, ch
 }  // namespace
 
 size_t code_linear_workspace(const mca_code_linear_args& a) {
+  if (use_pair(a)) return code_linear_pair_workspace(a);
   size_t n = 0;
-  if (!aligned(a.x, a.rows, a.ldx)) n += align256((size_t)a.rows * (size_t)round16(a.n_in));
-  if (!aligned(a.w, a.n_out, a.ldw)) n += align256((size_t)a.n_out * (size_t)round16(a.n_in));
+  if (!code_rows_aligned(a.x, a.rows, a.ldx)) n += align256((size_t)a.rows * (size_t)round16(a.n_in));
+  if (!code_rows_aligned(a.w, a.n_out, a.ldw)) n += align256((size_t)a.n_out * (size_t)round16(a.n_in));
   return n;
 }
 
 cudaError_t launch_code_linear(const mca_code_linear_args& args, cudaStream_t s) {
+  if (use_pair(args)) return launch_code_linear_pair(args, s);
   mca_code_linear_args a = args;
   char* ws = static_cast<char*>(a.workspace);
   cudaError_t e = align_rows(&a.x, a.rows, a.n_in, &a.ldx, &ws, s);

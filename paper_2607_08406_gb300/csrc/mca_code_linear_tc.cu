@@ -1,9 +1,9 @@
-// A layer on 8-bit codes for few samples, on the tensor cores: 128 outputs by up to 128 samples per CTA, the columns split
+// A layer on 8-bit codes for few samples, on the tensor cores: 128 outputs by up to 64 samples per CTA, the columns split
 // over the CTAs of a cluster where tiles are few.
 //
 // The transposed tile D[128 outputs x T samples] = W X^T is what a CTA computes, so that the weights, which are
 // most of what is read, are the A operand. TMA brings stages of 128 columns of both code matrices into a ring
-// in shared memory; four warps turn the weights' codes into fp16 in registers and store them to tensor memory (a
+// in shared memory; eight warps turn the weights' codes into fp16 in registers and store them to tensor memory (a
 // thread per row, 64 columns at a time), four others the samples' codes into the core-matrix layout of the B
 // operand in shared memory; one thread issues the MMAs. Weights thus pass through shared memory once as bytes and
 // are read back once, which is what limits the rate at which a CTA may take them.
@@ -16,25 +16,20 @@
 #include <algorithm>
 
 #include "mca_code_linear.cuh"
-#include "mca_tc.cuh"
 
 namespace mca {
 
 namespace {
 
-constexpr int kM = 128;                       // outputs per CTA (MMA M)
-constexpr int kRawK = 128;                    // columns per stage of the ring
-constexpr int kSubK = 64;                     // columns per converted operand
-constexpr int kThreads = 320;                 // warps 0-3 convert W, 4-7 X, 8 copies, 9 MMAs
-constexpr uint32_t kRawW = kM * kRawK;        // bytes
-constexpr uint32_t kColsA = kSubK / 2;        // tensor-memory columns of a converted W (two fp16 each)
+constexpr int kThreads = 448;                 // warps 0-7 convert W, 8-11 X, 12 copies, 13 MMAs
+constexpr int kCopyWarp = 12, kMmaWarp = 13;
 
 // T: most samples per tile. NR stages of raw codes, NC of converted ones. (256 tensor-memory columns and
 // less than half of the shared memory, so that two CTAs share an SM.)
 template <int T>
 struct Shape {
-  static constexpr int NR = T > 64 ? 2 : 4;
-  static constexpr int NC = T > 64 ? 2 : 4;
+  static constexpr int NR = T > 32 ? 3 : 4;
+  static constexpr int NC = T > 32 ? 3 : 4;
   static constexpr uint32_t kRaw = kRawW + T * kRawK;
   static constexpr uint32_t kConv = T * kSubK * 2;
   static constexpr uint32_t kSmem = NR * kRaw + NC * kConv + 1024;
@@ -46,68 +41,6 @@ struct SplitArgs {
   int box;                                    // samples per box of x's map, a multiple of 16
 };
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;"
-               ::: "memory");
-}
-__device__ __forceinline__ int ld_cluster(uint32_t addr, uint32_t rank) {
-  uint32_t a;
-  int v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
-               : "memory");
-}
-
-// 64 codes of a row (row r of a swizzled box at base, columns 64 half ..) as 32 pairs of fp16.
-__device__ __forceinline__ void load_codes(uint32_t base, int r, int half, uint32_t (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint4 q = lds128(base + (uint32_t)r * kRawK + (uint32_t)(((half * 4 + j) ^ (r & 7)) << 4));
-    codes_f16(q.x, v[8 * j], v[8 * j + 1]);
-    codes_f16(q.y, v[8 * j + 2], v[8 * j + 3]);
-    codes_f16(q.z, v[8 * j + 4], v[8 * j + 5]);
-    codes_f16(q.w, v[8 * j + 6], v[8 * j + 7]);
-  }
-}
-
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
-        "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
-        "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]),
-        "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]),
-        "r"(v[31])
-      : "memory");
-}
-
-template <int DT>
-__device__ __forceinline__ void write_output(const mca_code_linear_args& a, int64_t r, int n, int s,
-                                             float ws, float b) {
-  static_cast<elem_t<DT>*>(a.y)[r * a.ldy + n] = elem_of<DT>(
-      code_output(s, __ldg(a.x_scale + r), ws, b, a.bias != nullptr, a.act, a.act_param));
-}
-
 template <int T, int DT>
 __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
     const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, SplitArgs p) {
@@ -118,7 +51,7 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
   const mca_code_linear_args& a = p.a;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = tid >> 5;
   const int rank = p.splits > 1 ? (int)cluster_rank() : 0;
   const int tile = (int)(blockIdx.x / p.splits), ntiles = (a.n_out + kM - 1) / kM;
   const int n0 = tile % ntiles * kM;
@@ -131,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
   const uint32_t raw = (smem_u32(dyn) + 1023u) & ~1023u;
   const uint32_t conv = raw + S::NR * S::kRaw;
 
-  if (warp == 8) {
+  if (warp == kCopyWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;"
                  ::"r"(smem_u32(&s_tmem)));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -139,10 +72,10 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
   if (tid == 0) {
     for (int q = 0; q < S::NR; ++q) {
       mbar_init(&s_rawfull[q], 1);
-      mbar_init(&s_rawfree[q], 8);
+      mbar_init(&s_rawfree[q], kCopyWarp);     // the converting warps
     }
     for (int q = 0; q < S::NC; ++q) {
-      mbar_init(&s_full[q], 8);
+      mbar_init(&s_full[q], kCopyWarp / 2);
       mbar_init(&s_free[q], 1);
     }
     mbar_init(&s_sum, 1);
@@ -162,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
   for (int q = 0; q < kAcc; ++q) acc[q] = 0;
   const int half = warp >> 2;                              // of the samples, in the warps 0-7
 
-  if (warp == 8) {
+  if (warp == kCopyWarp) {
     if (elect_one()) {
       int issued = 0;
       for (int c = 0; c < nst; ++c) {
@@ -182,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
       for (int c = issued > S::NR ? issued - S::NR : 0; c < issued; ++c)
         if (!mbar_wait(&s_rawfull[c % S::NR], (uint32_t)(c / S::NR) & 1u)) s_fail = 1;
     }
-  } else if (warp == 9) {
+  } else if (warp == kMmaWarp) {
     if (elect_one()) {
       const uint32_t idesc = tc_idesc_f16(kM, 16) + ((uint32_t)((n16 >> 3) - 2) << 17);
       for (int u = 0; u < 2 * nst; ++u) {
@@ -207,58 +140,41 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
       }
     }
   } else {
-    const int row = tid & 127;
+    // stage c holds two operands' columns; half of the warps convert the first, half the second
+    const bool isx = warp >= 8;
+    const int h = isx ? (warp - 8) >> 1 : warp >> 2;
+    const int row = isx ? tid & 63 : tid & 127;
     bool ok = true;
     for (int c = 0; c < nst && ok; ++c) {
-      const int st = c % S::NR;
-      const uint32_t at = raw + (uint32_t)st * S::kRaw + (half ? kRawW : 0u);
-      ok = mbar_wait(&s_rawfull[st], (uint32_t)(c / S::NR) & 1u);
-      if (!__all_sync(0xffffffffu, ok)) {
-        ok = false;
-        break;
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int u = 2 * c + h, cs = u % S::NC;
-        uint32_t v[32];
-        if (!half || row < n16) load_codes(at, row, h, v);
-        if (h == 1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&s_rawfree[st]);
-        }
-        if (u >= S::NC) {
-          ok = mbar_wait(&s_free[cs], (uint32_t)(u / S::NC - 1) & 1u);
-          if (!__all_sync(0xffffffffu, ok)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-        }
-        if (half == 0) {
-          tmem_st32(tmem_a + (uint32_t)cs * kColsA + ((uint32_t)(warp * 32) << 16), v);
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          tc_fence_before();
-        } else {
-          if (row < n16) {
-            const uint32_t to = conv + (uint32_t)cs * S::kConv + (uint32_t)(row >> 3) * 128u +
-                                (uint32_t)(row & 7) * 16u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              sts128(to + (uint32_t)j * (T / 8) * 128u, v[4 * j], v[4 * j + 1], v[4 * j + 2],
-                     v[4 * j + 3]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s_full[cs]);
-      }
+      const int st = c % S::NR, u = 2 * c + h, cs = u % S::NC;
+      const uint32_t at = raw + (uint32_t)st * S::kRaw + (isx ? kRawW : 0u);
+      ok = warp_all(mbar_wait(&s_rawfull[st], (uint32_t)(c / S::NR) & 1u));
+      if (ok && u >= S::NC) ok = warp_all(mbar_wait(&s_free[cs], (uint32_t)(u / S::NC - 1) & 1u));
       if (!ok) break;
-      if (c % kPer == kPer - 1 || c == nst - 1) {          // an exact sum is complete
-        ok = mbar_wait(&s_sum, (uint32_t)(c / kPer) & 1u);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
+      tc_fence_after();
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint32_t v[16];
+        if (!isx) {
+          load_codes(at, row, 2 * h + part, v);
+          tmem_st16u(tmem_a + (uint32_t)cs * kColsA + (uint32_t)part * 16u +
+                         ((uint32_t)((warp & 3) * 32) << 16), v);
+        } else if (row < n16) {
+          load_codes(at, row, 2 * h + part, v);
+          store_codes(conv + (uint32_t)cs * S::kConv, row, T, part, v);
         }
+      }
+      warp_arrive(&s_rawfree[st]);
+      if (!isx) {
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+      } else {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      warp_arrive(&s_full[cs]);
+      if (!isx && (c % kPer == kPer - 1 || c == nst - 1)) {   // an exact sum is complete
+        ok = warp_all(mbar_wait(&s_sum, (uint32_t)(c / kPer) & 1u));
+        if (!ok) break;
         tc_fence_after();
         const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kAcc);
 #pragma unroll
@@ -267,60 +183,56 @@ __global__ void __launch_bounds__(kThreads, 2) code_linear_split_kernel(
             float d[16];
             tmem_ld16(from + (uint32_t)q, d);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (q + i < kAcc) acc[q + i] += __float2int_rn(d[i]);
+            for (int i = 0; i < 16; ++i) acc[q + i] += __float2int_rn(d[i]);
           }
         }
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s_taken);
+        warp_arrive(&s_taken);
       }
     }
+    // every MMA's arrival comes before the CTA leaves
+    for (int u = max(0, 2 * nst - S::NC); u < 2 * nst && ok; ++u)
+      ok = warp_all(mbar_wait(&s_free[u % S::NC], (uint32_t)(u / S::NC) & 1u));
     if (!ok) s_fail = 1;
   }
   __syncwarp();
   __syncthreads();
   const bool fail = s_fail != 0;
   const int ch = tid & 127, n = n0 + ch;
-  const bool mine = tid < 256 && n < a.n_out;
-  const float ws = mine ? __ldg(a.w_scale + n) : 0.0f;
-  const float b = mine && a.bias ? __ldg(a.bias + n) : 0.0f;
-  if (p.splits == 1) {
-    if (mine) {
+  // the parts of the cluster's CTAs, [sample][output], in the place of the rings
+  if (tid < 256) {
 #pragma unroll
-      for (int q = 0; q < kAcc; ++q) {
-        const int t = half * kAcc + q;
-        if (t < nt && !fail) write_output<DT>(a, r0 + t, n, acc[q], ws, b);
-      }
-    }
-  } else {
-    // the parts of the cluster's CTAs, [sample][output], in the place of the rings
-    if (tid < 256) {
-#pragma unroll
-      for (int q = 0; q < kAcc; ++q)
-        if (half * kAcc + q < nt)
-          asm volatile("st.shared.s32 [%0], %1;"
-                       ::"r"(raw + (uint32_t)((half * kAcc + q) * kM + ch) * 4u), "r"(acc[q])
-                       : "memory");
-    }
+    for (int q = 0; q < kAcc; ++q)
+      if (half * kAcc + q < nt)
+        asm volatile("st.shared.s32 [%0], %1;"
+                     ::"r"(raw + (uint32_t)((half * kAcc + q) * kM + ch) * 4u), "r"(acc[q])
+                     : "memory");
+  }
+  if (p.splits > 1)
     cluster_sync_all();
-    if (mine && !fail) {
-      for (int t = rank * 2 + half; t < nt; t += 2 * p.splits) {
-        int s = 0;
+  else
+    __syncthreads();
+  if (tid < 256 && n < a.n_out) {
+    const float ws = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.0f;
+    elem_t<DT>* y = static_cast<elem_t<DT>*>(a.y) + r0 * a.ldy + n;
+    // any CTA of a cluster that failed: its part is missing in every sample
+    for (int t = fail ? half : rank * 2 + half; t < nt; t += fail ? 2 : 2 * p.splits) {
+      int s = 0;
+      if (p.splits > 1)
         for (int q = 0; q < p.splits; ++q) s += ld_cluster(raw + (uint32_t)(t * kM + ch) * 4u, q);
-        write_output<DT>(a, r0 + t, n, s, ws, b);
-      }
+      else
+        s = ld_shared(raw + (uint32_t)(t * kM + ch) * 4u);
+      const float z = code_field(__int2float_rn(s), __ldg(a.x_scale + r0 + t), ws, b, a.bias != nullptr);
+      y[t * a.ldy] = elem_of<DT>(fail ? NAN : act_accurate(a.act, z, a.act_param));
     }
   }
-  if (fail && mine)                        // any CTA of a cluster: its part is missing in every sample
-    for (int t = half; t < nt; t += 2)
-      static_cast<elem_t<DT>*>(a.y)[(r0 + t) * a.ldy + n] = elem_of<DT>(NAN);
   tc_fence_before();
   if (p.splits > 1)
     cluster_sync_all();
   else
     __syncthreads();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem));
+  if (warp == kCopyWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem));
 }
 
 template <int T, int DT>
@@ -360,7 +272,7 @@ cudaError_t launch_split_t(const SplitArgs& p, const CUtensorMap& wmap, const CU
 }  // namespace
 
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s) {
-  const int T = a.rows <= 32 ? 32 : 128;
+  const int T = a.rows <= 32 ? 32 : 64;
   SplitArgs p{};
   p.a = a;
   p.stages = (a.n_in + kRawK - 1) / kRawK;
@@ -373,7 +285,7 @@ cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t
   cudaError_t e = code_map(&wmap, a.w, a.n_out, a.n_in, a.ldw, kM);
   if (e == cudaSuccess) e = code_map(&xmap, a.x, a.rows, a.n_in, a.ldx, p.box);
   if (e != cudaSuccess) return e;
-  return T == 32 ? launch_split_t<32>(p, wmap, xmap, s) : launch_split_t<128>(p, wmap, xmap, s);
+  return T == 32 ? launch_split_t<32>(p, wmap, xmap, s) : launch_split_t<64>(p, wmap, xmap, s);
 }
 
 }  // namespace mca

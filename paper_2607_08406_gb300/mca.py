@@ -535,8 +535,7 @@ def _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype
 
 def mca_code_linear_workspace_size(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity",
                                    act_param: float = 0.0, dtype=None) -> int:
-    """Bytes of workspace of mca_code_linear (0 where the rows of both operands start on 16-byte
-    boundaries)."""
+    """Bytes of workspace of mca_code_linear for these operands."""
     a = _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype)
     n = c_size_t(0)
     _check(load_library().mca_code_linear_workspace_size(ctypes.byref(a), ctypes.byref(n)))
