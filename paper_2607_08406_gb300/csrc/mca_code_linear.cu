@@ -6,9 +6,13 @@ namespace mca {
 
 namespace {
 
-constexpr int64_t kPairRows = 128;
+enum class Kernel { kStream, kSplit, kPair };
 
-bool use_pair(const mca_code_linear_args& a) { return a.rows > kPairRows; }
+Kernel choose(const mca_code_linear_args& a) {
+  const double w = (double)a.n_in * a.n_out;
+  if (a.rows <= 32 || (a.rows <= 64 && w <= 16e6) || (a.rows <= 256 && w <= 1.1e6)) return Kernel::kStream;
+  return a.rows > 96 ? Kernel::kPair : Kernel::kSplit;
+}
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -46,7 +50,7 @@ cudaError_t align_rows(const int8_t** p, int64_t rows, int cols, int64_t* ld, ch
 }  // namespace
 
 size_t code_linear_workspace(const mca_code_linear_args& a) {
-  if (use_pair(a)) return code_linear_pair_workspace(a);
+  if (choose(a) == Kernel::kPair) return code_linear_pair_workspace(a);
   size_t n = 0;
   if (!code_rows_aligned(a.x, a.rows, a.ldx)) n += align256((size_t)a.rows * (size_t)round16(a.n_in));
   if (!code_rows_aligned(a.w, a.n_out, a.ldw)) n += align256((size_t)a.n_out * (size_t)round16(a.n_in));
@@ -54,40 +58,13 @@ size_t code_linear_workspace(const mca_code_linear_args& a) {
 }
 
 cudaError_t launch_code_linear(const mca_code_linear_args& args, cudaStream_t s) {
-  if (use_pair(args)) return launch_code_linear_pair(args, s);
+  if (choose(args) == Kernel::kPair) return launch_code_linear_pair(args, s);
   mca_code_linear_args a = args;
   char* ws = static_cast<char*>(a.workspace);
   cudaError_t e = align_rows(&a.x, a.rows, a.n_in, &a.ldx, &ws, s);
   if (e == cudaSuccess) e = align_rows(&a.w, a.n_out, a.n_in, &a.ldw, &ws, s);
   if (e != cudaSuccess) return e;
-  return launch_code_linear_split(a, s);
-}
-
-cudaError_t code_map(CUtensorMap* map, const int8_t* p, int64_t rows, int64_t cols, int64_t ld,
-                     int box_rows) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                              CUtensorMapFloatOOBfill);
-  static const Encode encode = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) !=
-            cudaSuccess ||
-        r != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      f = nullptr;
-    }
-    return reinterpret_cast<Encode>(f);
-  }();
-  if (!encode) return cudaErrorNotSupported;
-  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t stride[1] = {(cuuint64_t)(rows == 1 ? round16(cols) : ld)};
-  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, step[2] = {1, 1};
-  const CUresult e = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p), dim, stride, box,
-                            step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return e == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+  return choose(a) == Kernel::kStream ? launch_code_linear_stream(a, s) : launch_code_linear_split(a, s);
 }
 
 }  // namespace mca

@@ -1,12 +1,10 @@
-// What the kernels of mca_code_linear share: the output of an integer sum, codes as fp16, tensor maps.
+// What the kernels of mca_code_linear share: the output of an integer sum, codes as fp16.
 //
 // An 8-bit code is an fp16 number exactly, products of two are integers below 2^14, and a sum of 1024 of them
 // stays within 2^24 = 128 * 128 * 1024, so that kind::f16 MMAs accumulate it exactly in fp32: sm_103a has no
 // tcgen05 form for 8-bit integers, and mma.sync's is slow. Longer sums are taken out of tensor memory after every
 // 1024 columns (kExactK) and added up as integers.
 #pragma once
-
-#include <cuda.h>
 
 #include "mca_answers.h"
 #include "mca_elem.cuh"
@@ -16,10 +14,6 @@ namespace mca {
 
 constexpr int kExactK = 1024;
 constexpr int kM = 128;                       // outputs per CTA (a CTA's rows of the MMA's M)
-constexpr int kRawK = 128;                    // columns per stage of raw codes
-constexpr int kSubK = 64;                     // columns per converted operand
-constexpr uint32_t kRawW = kM * kRawK;        // bytes
-constexpr uint32_t kColsA = kSubK / 2;        // tensor-memory columns of a converted W (two fp16 each)
 
 // The transfer functions as they are defined, for outputs that a caller sees: relative accuracy near 0 and
 // for small tails, which the trial loop's forms (mca_device.cuh) leave out. NaN stays NaN.
@@ -31,6 +25,25 @@ __device__ __forceinline__ float act_accurate(int act, float z, float g) {
     case MCA_ACT_GAUSSIAN: return expf(-g * z * z);
     case MCA_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
     default: return z;
+  }
+}
+
+template <int ACT, int N>
+__device__ __forceinline__ void act_block(float (&v)[N], float g) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = act_accurate(ACT, v[i], g);
+}
+// The same for a block of fields: one branch for all (left to each field, the compiler evaluates every function and
+// selects: 400 cycles an output).
+template <int N>
+__device__ __forceinline__ void act_block(float (&v)[N], int act, float g) {
+  if (act == MCA_ACT_IDENTITY) return;
+  switch (act) {
+    case MCA_ACT_TANH: act_block<MCA_ACT_TANH>(v, g); break;
+    case MCA_ACT_SIGMOID: act_block<MCA_ACT_SIGMOID>(v, g); break;
+    case MCA_ACT_RELU: act_block<MCA_ACT_RELU>(v, g); break;
+    case MCA_ACT_GAUSSIAN: act_block<MCA_ACT_GAUSSIAN>(v, g); break;
+    default: act_block<MCA_ACT_GELU>(v, g); break;
   }
 }
 
@@ -74,36 +87,24 @@ __device__ __forceinline__ int ld_shared(uint32_t a) {
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
                : "memory");
 }
 
-// 32 codes of a row (row r of a swizzled box at base, columns 32 part ..) as 16 pairs of fp16.
-__device__ __forceinline__ void load_codes(uint32_t base, int r, int part, uint32_t (&v)[16]) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const uint4 q = lds128(base + (uint32_t)r * kRawK + (uint32_t)(((part * 2 + j) ^ (r & 7)) << 4));
-    codes_f16(q.x, v[8 * j], v[8 * j + 1]);
-    codes_f16(q.y, v[8 * j + 2], v[8 * j + 3]);
-    codes_f16(q.z, v[8 * j + 4], v[8 * j + 5]);
-    codes_f16(q.w, v[8 * j + 6], v[8 * j + 7]);
+// 16 codes of a row (on a 16-byte boundary) from column k; zeros behind column n, which is not read beyond.
+__device__ __forceinline__ uint4 load_codes16(const int8_t* p, int k, int n) {
+  if (k + 16 <= n) {
+    uint4 v;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p + k));
+    return v;
   }
-}
-
-// The same into the core-matrix layout of an operand of `rows` rows at `to`: units of 8 columns rows * 16 bytes
-// apart (part: of the operand's columns).
-__device__ __forceinline__ void store_codes(uint32_t to, int r, int rows, int part, const uint32_t (&v)[16]) {
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    sts128(to + (uint32_t)((part * 4 + j) * rows + r) * 16u, v[4 * j], v[4 * j + 1], v[4 * j + 2],
-           v[4 * j + 3]);
+  for (int i = 0; i < 16; ++i)
+    if (k + i < n) w[i >> 2] |= (uint32_t)(uint8_t)p[k + i] << (8 * (i & 3));
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // One lane of a converged warp arrives; the warp stays converged for the tensor-memory instructions.
@@ -119,36 +120,13 @@ __device__ __forceinline__ bool warp_all(bool ok) {
   return ok;
 }
 
-__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
-        "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
-        "r"(v[15])
-      : "memory");
-}
-
-// One thread: a box of a 2-D tensor map (x: byte column, a multiple of 16; y: row) into shared memory;
-// elements outside the matrix arrive as zeros. Completes bytes on bar.
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%2, %3}], [%4];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
-// Map of a code matrix [rows x cols], row distance ld (a multiple of 16, base too), in boxes of box_rows
-// x 128 bytes whose 16-byte units are stored exchanged (128-byte swizzle: unit j of row r at j ^ (r % 8)).
-cudaError_t code_map(CUtensorMap* map, const int8_t* p, int64_t rows, int64_t cols, int64_t ld,
-                     int box_rows);
-
 // Rows that start on 16-byte boundaries.
 inline bool code_rows_aligned(const int8_t* p, int64_t rows, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || ld % 16 == 0);
 }
 
+// mca_code_linear_stream.cu: few samples; operands' rows on 16-byte boundaries.
+cudaError_t launch_code_linear_stream(const mca_code_linear_args& a, cudaStream_t s);
 // mca_code_linear_tc.cu: few samples; operands' rows on 16-byte boundaries.
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s);
 // mca_code_linear_pair.cu: many samples; in a.workspace the operands as fp16.

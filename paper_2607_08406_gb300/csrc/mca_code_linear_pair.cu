@@ -29,6 +29,7 @@ constexpr int kTB = 128;                        // samples per CTA
 constexpr int kT = 2 * kTB;                     // samples per tile (MMA N)
 constexpr int kPairThreads = 384;
 constexpr int kFirstSum = 4;                    // first warp of those that take the sums
+constexpr int kSubK = 64;                       // columns per chunk
 constexpr int kStages = 6;
 constexpr uint32_t kChunk = kM * kSubK * 2;     // bytes of a block's chunk of 64 columns
 constexpr uint32_t kStage = 2 * kChunk;
@@ -145,18 +146,13 @@ __device__ __forceinline__ void tile_at(const PairArgs& p, int i, int* n0, int64
   *r0 = (int64_t)(k / gn) * kT;
 }
 
-template <int ACT>
-__device__ __forceinline__ void act16(float (&v)[16], float g) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = act_accurate(ACT, v[i], g);
-}
-
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     code_linear_pair_kernel(PairArgs p) {
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_free[kStages], s_sum[2], s_taken[2];
   __shared__ uint32_t s_tmem;
+  __shared__ float s_scale[8][kTB];             // of a tile's samples, for each warp that takes sums
   const mca_code_linear_args& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_rank();
@@ -261,6 +257,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const int n = n0 + rank * kM + (warp & 3) * 32 + lane;
       r0 += half * kTB;
       const int nt = (int)max((int64_t)0, min((int64_t)kTB, a.rows - r0));
+      float* const xs = s_scale[warp - kFirstSum];
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < kTB; q += 32)
+        if (q + lane < nt) xs[q + lane] = __ldg(a.x_scale + r0 + q + lane);
+      __syncwarp();
       uint32_t from = 0u;
       if (nsum == 1) {
         ok = ok && warp_all(wait_pair(&s_sum[d & 1], (uint32_t)(d >> 1) & 1u));
@@ -309,24 +311,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           tmem_ld16(from + (uint32_t)q, v);
 #pragma unroll
           for (int k = 0; k < 16; ++k)
-            v[k] = code_field(v[k], __ldg(a.x_scale + min(r0 + q + k, a.rows - 1)), ws, b,
-                              a.bias != nullptr);
-          switch (a.act) {
-            case MCA_ACT_TANH: act16<MCA_ACT_TANH>(v, a.act_param); break;
-            case MCA_ACT_SIGMOID: act16<MCA_ACT_SIGMOID>(v, a.act_param); break;
-            case MCA_ACT_RELU: act16<MCA_ACT_RELU>(v, a.act_param); break;
-            case MCA_ACT_GAUSSIAN: act16<MCA_ACT_GAUSSIAN>(v, a.act_param); break;
-            case MCA_ACT_GELU: act16<MCA_ACT_GELU>(v, a.act_param); break;
-            default: break;
-          }
+            v[k] = code_field(v[k], xs[q + k], ws, b, a.bias != nullptr);
+          act_block(v, a.act, a.act_param);
         } else {
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = NAN;
         }
         if (live) {
+          if (q + 16 <= nt) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k)
-            if (q + k < nt) y[(q + k) * a.ldy] = elem_of<DT>(v[k]);
+            for (int k = 0; k < 16; ++k, y += a.ldy) *y = elem_of<DT>(v[k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k, y += a.ldy)
+              if (q + k < nt) *y = elem_of<DT>(v[k]);
+          }
         }
         __syncwarp();
       }

@@ -39,4 +39,11 @@ __device__ __forceinline__ elem_t<DT> elem_of(float v) {
     return __float2bfloat16_rn(v);
 }
 
+constexpr float kRound = 12582912.0f;         // 1.5 * 2^23: x + kRound rounds |x| <= 2^22 to an integer,
+constexpr int kRoundBits = 0x4B400000;        // whose bits follow those of kRound
+
+// The integer next to x (halves to the even one), |x| <= 2^22, as an integer and as fp32.
+__device__ __forceinline__ int near_int(float x) { return __float_as_int(__fadd_rn(x, kRound)) - kRoundBits; }
+__device__ __forceinline__ float near_f32(float x) { return __fsub_rn(__fadd_rn(x, kRound), kRound); }
+
 }  // namespace mca

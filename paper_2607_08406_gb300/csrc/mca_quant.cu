@@ -31,14 +31,14 @@ __device__ __forceinline__ RowScale row_scale(float s) {
 __device__ __forceinline__ int code_of(float x, const RowScale& r) {
   const float a = fabsf(x) * r.up;
   const float t = a * r.inv;
-  float c = rintf(t);
-  const float f = floorf(t);
-  if (fabsf(t - f - 0.5f) < 1e-4f) {
+  float c = near_f32(t);
+  if (fabsf(t - c) > 0.4999f) {
+    const float f = c <= t ? c : c - 1.0f;                      // the half is f + 1/2
     const float d = fmaf(-(f + 0.5f), r.s, a);
-    c = d > 0.0f || (d == 0.0f && ((int)f & 1)) ? f + 1.0f : f;
+    c = d > 0.0f || (d == 0.0f && (near_int(f) & 1)) ? f + 1.0f : f;
   }
   c = fminf(c, 127.0f);            // a scale that was rounded down to a subnormal number
-  return (int)(x < 0.0f ? -c : c);
+  return near_int(copysignf(c, x));
 }
 
 // Sixteen bytes of elements, or one element where rows lie off 16-byte boundaries.
