@@ -452,7 +452,7 @@ mca_status mca_code_linear(const mca_code_linear_args* a);
 typedef struct {
   const void* logits;      /* [rows x vocab] of `dtype` */
   int32_t dtype;           /* mca_dtype */
-  int32_t vocab;           /* >= 1 */
+  int32_t vocab;           /* 1..2^30 */
   int64_t rows, ld;
   const int32_t* targets;  /* [rows]; nullable where logprob is */
   float* logprob;          /* [rows], nullable: logits[r, targets[r]] - lse[r] */

@@ -323,7 +323,8 @@ mca_status mca_token_logprobs(const mca_token_logprobs_args* a) {
   if (!a) return fail(nullptr, MCA_ERR_INVALID, "NULL argument");
   MCA_CHECK(check_dtype(a->dtype));
   MCA_CHECK(check_rows(nullptr, a->rows));
-  if (a->vocab < 1) return fail(nullptr, MCA_ERR_INVALID, "vocab = %d", a->vocab);
+  if (a->vocab < 1 || a->vocab > 1 << 30)
+    return fail(nullptr, MCA_ERR_INVALID, "vocab = %d outside 1..2^30", a->vocab);
   MCA_CHECK(check_matrix(nullptr, "logits", a->rows, a->vocab, a->ld));
   if (a->rows == 0) return MCA_OK;
   MCA_CHECK(check_logprobs(*a, nullptr));
@@ -335,7 +336,8 @@ mca_status mca_token_logprobs_backward(const mca_token_logprobs_backward_args* a
   if (!a) return fail(nullptr, MCA_ERR_INVALID, "NULL argument");
   MCA_CHECK(check_dtype(a->dtype));
   MCA_CHECK(check_rows(nullptr, a->rows));
-  if (a->vocab < 1) return fail(nullptr, MCA_ERR_INVALID, "vocab = %d", a->vocab);
+  if (a->vocab < 1 || a->vocab > 1 << 30)
+    return fail(nullptr, MCA_ERR_INVALID, "vocab = %d outside 1..2^30", a->vocab);
   MCA_CHECK(check_matrix(nullptr, "logits", a->rows, a->vocab, a->ld));
   MCA_CHECK(check_matrix(nullptr, "grad", a->rows, a->vocab, a->ldg));
   if (a->rows == 0) return MCA_OK;
