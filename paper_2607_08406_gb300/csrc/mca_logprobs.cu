@@ -7,8 +7,10 @@
 // product per logit. What bounds them is the memory: 2048 x 50001 bf16, 0.2 GB, takes 30 us at 6.8 TB/s.
 //
 // Alternatives without a second pass: a thread remembers in which of its 16-byte pieces its largest logit was (one
-// comparison a piece). The k-th largest of the threads' largest is a bound that the k-th alternative cannot be below,
-// and just k threads reach it, so that only their pieces are read again (from L2).
+// comparison a piece). The threads' largest give a bound that the k-th alternative cannot be below, and not many
+// more than k threads reach it, so that only their pieces are read again (from L2). What is found there is few
+// enough to be put in order by counting. (Sorting the threads' largest and merging lists over the CTA took 9 us of a
+// row's 25.)
 #include <algorithm>
 
 #include "mca_answers.h"
@@ -160,6 +162,9 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary (a CTA's threads have no piece each),
+constexpr int kWarpVocab = 8192;          //   up to this one from
+constexpr int kWarpRows = 1024;           //   so many rows
 
 // A row's 16-byte pieces: piece j holds the logits j N - head .. of the row (the first and the last in part).
 template <int DT>
@@ -173,9 +178,8 @@ struct Pieces {
   }
   __device__ __forceinline__ int index(int j, int i) const { return j * N - head + i; }
   __device__ __forceinline__ bool whole(int j) const { return j * N >= head && (int64_t)(j + 1) * N <= (int64_t)V + head; }
-  __device__ __forceinline__ uint4 raw(int j) const {
-    return *reinterpret_cast<const uint4*>(x + (int64_t)j * N - head);
-  }
+  __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(x - head); }
+  __device__ __forceinline__ uint4 raw(int j) const { return pieces()[j]; }
   __device__ __forceinline__ static void values(const uint4& q, float (&v)[N]) {
     const unsigned int w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -189,49 +193,23 @@ struct Pieces {
     }
   }
   // Any piece of the row, -inf in the place of what is outside.
-  __device__ __forceinline__ void load(int j, float (&v)[N]) const {
-    if (whole(j)) {
-      values(raw(j), v);
-      return;
-    }
+  __device__ __forceinline__ uint4 bits(int j) const {
+    return whole(j) ? raw(j) : part(j);
+  }
+  __device__ __noinline__ uint4 part(int j) const {
+    union {
+      elem_t<DT> e[N];
+      uint4 u;
+    } o;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t q = (int64_t)j * N - head + i;
-      v[i] = q >= 0 && q < V ? elem_f32(x[q]) : -INFINITY;
+      const int q = index(j, i);
+      o.e[i] = q >= 0 && q < V ? x[q] : elem_of<DT>(-INFINITY);
     }
+    return o.u;
   }
+  __device__ __forceinline__ void load(int j, float (&v)[N]) const { values(bits(j), v); }
 };
-
-__device__ __forceinline__ Key exchange(Key k, int j, bool larger) {
-  const Key q = __shfl_xor_sync(0xffffffffu, k, j);
-  return (q > k) == larger ? q : k;
-}
-// A warp's keys in falling order.
-__device__ __forceinline__ Key warp_sort(Key k) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int n = 2; n <= 32; n <<= 1)
-#pragma unroll
-    for (int j = n >> 1; j > 0; j >>= 1) k = exchange(k, j, ((lane & j) == 0) == ((lane & n) == 0));
-  return k;
-}
-// The 32 largest of two lists in falling order.
-__device__ __forceinline__ Key warp_merge(Key k, Key reversed) {
-  const int lane = threadIdx.x & 31;
-  k = reversed > k ? reversed : k;
-#pragma unroll
-  for (int j = 16; j > 0; j >>= 1) k = exchange(k, j, (lane & j) == 0);
-  return k;
-}
-// The 32 largest of n lists (a power of two, at most kWarps), into the first. The whole CTA.
-__device__ __forceinline__ void merge_lists(Key (*list)[32], int n) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  __syncthreads();
-  for (n >>= 1; n > 0; n >>= 1) {
-    if (warp < n) list[warp][lane] = warp_merge(list[warp][lane], list[warp + n][31 - lane]);
-    __syncthreads();
-  }
-}
 
 __device__ __forceinline__ unsigned int cluster_rank() {
   unsigned int r;
@@ -253,153 +231,381 @@ __device__ __forceinline__ unsigned int first_cta(const void* p) {      // the a
   return a;
 }
 
+// A row's pass without special cases: what lies below `low` counts as low (-inf too), whose terms vanish beside a
+// largest logit above `high`. Rows without one, or with less than the asked alternatives above low, go through
+// exact_row instead.
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, int split) {
-  using P = Pieces<DT>;
-  __shared__ Sums s_sum[kWarps];
-  __shared__ Key s_list[kWarps][32];
-  __shared__ Sums s_part[kMaxCluster];
-  __shared__ Key s_best[kMaxCluster][32];
-  const mca_token_logprobs_args& a = p.a;
-  const int64_t r = blockIdx.x / split;
-  const int rank = split > 1 ? (int)cluster_rank() : 0;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const P row(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld, a.vocab);
-  const int j0 = (int)((int64_t)row.count * rank / split), j1 = (int)((int64_t)row.count * (rank + 1) / split);
+struct Range {
+  static constexpr float low = DT == MCA_DTYPE_FP16 ? -65504.0f : -0x1p100f;
+  static constexpr float high = DT == MCA_DTYPE_FP16 ? -65000.0f : -0x1p99f;
+};
 
-  if (split > 1) cluster_arrive();                              // every CTA runs before one writes to another
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 
-  // the pass: largest logit, where it was, sums
-  Sums sum{kLowest, 0.0f, 0.0f};
-  float top = -INFINITY;
-  int at = -1;
-  auto take = [&](const float (&v)[P::N], int j) {
-    float b = v[0];
+// A piece's logits, at least low (NaN stays), in pairs, and the largest (NaN left out).
+template <int DT>
+__device__ __forceinline__ float clamp_piece(const uint4& q, float2 (&v)[Pieces<DT>::N / 2]) {
+  unsigned int w[4] = {q.x, q.y, q.z, q.w};
+  if constexpr (DT == MCA_DTYPE_FP32) {
 #pragma unroll
-    for (int i = 1; i < P::N; ++i) b = fmaxf(b, v[i]);
+    for (int i = 0; i < 2; ++i)
+      v[i] = make_float2(max_nan(__uint_as_float(w[2 * i]), Range<DT>::low),
+                         max_nan(__uint_as_float(w[2 * i + 1]), Range<DT>::low));
+    return fmaxf(fmaxf(v[0].x, v[0].y), fmaxf(v[1].x, v[1].y));
+  } else if constexpr (DT == MCA_DTYPE_BF16) {
+    unsigned int m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                               // bf16 -2^100 is 0xf180
+      asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w[i]) : "r"(w[i]), "r"(0xf180f180u));
+      v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+    asm("{\n\t.reg .b32 a, b;\n\tmax.bf16x2 a, %1, %2;\n\tmax.bf16x2 b, %3, %4;\n\tmax.bf16x2 %0, a, b;\n\t}"
+        : "=r"(m) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  } else {
+    unsigned int m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                               // fp16 -65504 is 0xfbff
+      asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(w[i]) : "r"(w[i]), "r"(0xfbfffbffu));
+      v[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    }
+    asm("{\n\t.reg .b32 a, b;\n\tmax.f16x2 a, %1, %2;\n\tmax.f16x2 b, %3, %4;\n\tmax.f16x2 %0, a, b;\n\t}"
+        : "=r"(m) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return fmaxf(f.x, f.y);
+  }
+}
+
+// What a thread has seen. The sums refer to m, which follows the largest logit only when that is kLead above it (terms up
+// to e^kLead lose nothing), so that most pieces take no rescaling. Terms are added in pairs.
+constexpr float kLead = 8.0f;
+
+template <int DT>
+struct Seen {
+  float m = Range<DT>::low, top = Range<DT>::low;
+  int at = -1;                              // piece of the first logit of size top
+  float2 s = {0.0f, 0.0f}, u = {0.0f, 0.0f};
+  __device__ __forceinline__ void raise(float to) {
+    const float c = m - to, f = ex2_ftz(c * kLog2e);
+    u.x = f > 0.0f ? f * fmaf(s.x, c, u.x) : 0.0f;
+    u.y = f > 0.0f ? f * fmaf(s.y, c, u.y) : 0.0f;
+    s.x *= f;
+    s.y *= f;
+    m = to;
+  }
+  __device__ __forceinline__ void take(const uint4& q, int j) {
+    float2 v[Pieces<DT>::N / 2];
+    const float b = clamp_piece<DT>(q, v);
     if (b > top) {
       top = b;
       at = j;
+      if (b > m + kLead) raise(b);
     }
-    sum.raise(fmaxf(sum.m, b));
+    const float2 mm = make_float2(-m, -m), l2 = make_float2(kLog2e, kLog2e);
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) sum.add(v[i]);
-  };
-  int j = j0 + tid;
-  constexpr int kAhead = 4;
-  for (; j + (kAhead - 1) * kThreads < j1; j += kAhead * kThreads) {
-    float v[P::N];
-    if (row.whole(j) && row.whole(j + (kAhead - 1) * kThreads)) {
-      uint4 q[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) q[i] = row.raw(j + i * kThreads);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        P::values(q[i], v);
-        take(v, j + i * kThreads);
-      }
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < kAhead; ++i) {
-        row.load(j + i * kThreads, v);
-        take(v, j + i * kThreads);
-      }
+    for (int i = 0; i < Pieces<DT>::N / 2; ++i) {
+      const float2 d = add2(v[i], mm), p = mul2(d, l2), e = make_float2(ex2_ftz(p.x), ex2_ftz(p.y));
+      s = add2(s, e);
+      u = fma2(e, d, u);
     }
   }
-#pragma unroll 1
-  for (; j < j1; j += kThreads) {
-    float v[P::N];
-    row.load(j, v);
-    take(v, j);
+  // The sums relative to the largest logit.
+  __device__ __forceinline__ Sums sums() {
+    raise(fmaxf(top, m));
+    return {m, s.x + s.y, u.x + u.y};
   }
+};
 
-  // the CTA's sums
-  Sums all = sum;
+// A team of W warps has a row: a warp of a CTA's eight, or the CTA.
+template <int W>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (W == 1)
+    __syncwarp();
+  else
+    __syncthreads();
+}
+
+template <int W>
+struct Team {
+  static constexpr int kCand = W == 1 ? 64 : 512;
+  static_assert(kCand >= W * 32, "the lists of ordered_top");
+  Sums sum[W];
+  Key key[W];
+  int n;                                    // candidates
+  Key cand[kCand];
+};
+
+template <int W>
+__device__ __forceinline__ Sums team_sums(Sums t, Team<W>& s) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
-    all.join(__shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o),
-             __shfl_xor_sync(0xffffffffu, all.u, o));
-  if (lane == 0) s_sum[warp] = all;
+    t.join(__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o),
+           __shfl_xor_sync(0xffffffffu, t.u, o));
+  if constexpr (W > 1) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) s.sum[threadIdx.x >> 5] = t;
+    __syncthreads();
+    t = s.sum[lane % W];
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1)
+      t.join(__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o),
+             __shfl_xor_sync(0xffffffffu, t.u, o));
+  }
+  // the same number in every thread: join rounds by the side that it is called from
+  t.m = __shfl_sync(0xffffffffu, t.m, 0);
+  t.s = __shfl_sync(0xffffffffu, t.s, 0);
+  t.u = __shfl_sync(0xffffffffu, t.u, 0);
+  return t;
+}
 
-  // the CTA's alternatives
-  if (a.top > 0) {
-    Key key = 0ull;
-    if (at >= 0) {
-      float v[P::N];
-      row.load(at, v);
-#pragma unroll
-      for (int i = P::N - 1; i >= 0; --i)
-        if (v[i] == top) key = order_key(top, row.index(at, i));
-    }
-    if (a.top == 1) {
-      const Key b = group_max<32>(key);
-      s_list[warp][lane] = lane == 0 ? b : 0ull;
-    } else {
-      s_list[warp][lane] = warp_sort(key);
-    }
-    merge_lists(s_list, kWarps);
-    if (a.top > 1) {
-      const Key bound = s_list[0][a.top - 1];
+// Any row, by the definition: passes for the largest logit, for the sums and for every alternative.
+template <int DT, int W>
+__device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>& s) {
+  const mca_token_logprobs_args& a = p.a;
+  const elem_t<DT>* x = static_cast<const elem_t<DT>*>(a.logits) + r * a.ld;
+  const int tid = threadIdx.x % (32 * W), lane = tid & 31, warp = tid >> 5;
+  Sums t{kLowest, 0.0f, 0.0f};
+  for (int v = tid; v < a.vocab; v += 32 * W) t.m = fmaxf(t.m, elem_f32(x[v]));
+  for (int v = tid; v < a.vocab; v += 32 * W) t.add(elem_f32(x[v]));
+  __syncwarp();
+  team_sync<W>();
+  t = team_sums<W>(t, s);
+  if (tid == 0) write_row<DT>(p, r, x, t);
+  const Row w(t);
+  Key last = ~0ull;
+  for (int k = 0; k < a.top; ++k) {
+    Key best = 0ull;
+    if (last > 1ull)
+      for (int v = tid; v < a.vocab; v += 32 * W) {
+        const Key q = order_key(elem_f32(x[v]), v);
+        if (q < last && q > best) best = q;
+      }
+    __syncwarp();
+    best = group_max<32>(best);
+    if constexpr (W > 1) {
       __syncthreads();
-      Key mine = 0ull;                                          // the warp's list, in falling order
-      unsigned int todo = __ballot_sync(0xffffffffu, key >= bound && key != 0ull);
-      while (todo) {
-        const int owner = __ffs(todo) - 1;
-        todo &= todo - 1;
-        for (int b = j0 + warp * 32 + owner; b < j1; b += 32 * kThreads) {
-          const int jj = b + lane * kThreads;
-          float v[P::N];
+      if (lane == 0) s.key[warp] = best;
+      __syncthreads();
+      for (int q = 0; q < W; ++q) best = s.key[q] > best ? s.key[q] : best;
+    }
+    if (tid == 0) write_top(a, r, k, best, w);
+    last = best ? best : 1ull;
+  }
+}
+
+// The pieces of the threads whose largest logit reaches the bound, again: visit(key) for each logit that does. The whole
+// warp takes a thread's pieces, one per lane.
+template <int DT, int W, class Visit>
+__device__ __forceinline__ void revisit(const Pieces<DT>& row, int j0, int j1, Key key, Key bound, Visit visit) {
+  constexpr int N = Pieces<DT>::N;
+  const int lane = threadIdx.x & 31, first = threadIdx.x % (32 * W) - lane;
+  const float low = fmaxf(Range<DT>::low, bound ? key_value(bound) : -INFINITY);
+  unsigned int todo = __ballot_sync(0xffffffffu, key != 0ull && key >= bound);
+  while (todo) {
+    const int owner = __ffs(todo) - 1;
+    todo &= todo - 1;
+    for (int b = j0 + first + owner; b < j1; b += 32 * 32 * W) {
+      const int j = b + lane * 32 * W;
+      float v[N];
+      float m = -INFINITY;
+      if (j < j1) {
+        row.load(j, v);
 #pragma unroll
-          for (int i = 0; i < P::N; ++i) v[i] = -INFINITY;
-          if (jj < j1) row.load(jj, v);
+        for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
+      }
+      // (logits at or below the range's low: exact_row, if the row has no others)
+      const bool any = m >= low && m > Range<DT>::low;
+      if (__ballot_sync(0xffffffffu, any)) {
 #pragma unroll
-          for (int i = 0; i < P::N; ++i) {
-            const Key q = order_key(v[i], row.index(jj, i));
-            unsigned int found = __ballot_sync(0xffffffffu, q != 0ull && q >= bound);
-            while (found) {
-              const Key f = __shfl_sync(0xffffffffu, q, __ffs(found) - 1);
-              found &= found - 1;
-              const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
-              if (mine < f) mine = lane == 0 || above > f ? f : above;
-            }
-          }
+        for (int i = 0; i < N; ++i) {
+          const Key q = any && v[i] > Range<DT>::low ? order_key(v[i], row.index(j, i)) : 0ull;
+          visit(q != 0ull && q >= bound ? q : 0ull);
         }
       }
-      s_list[warp][lane] = mine;
-      merge_lists(s_list, kWarps);
     }
   }
-  __syncthreads();
+}
 
-  if (split > 1) {                                              // to the cluster's first CTA
-    cluster_wait();
-    if (warp == 0) {
-      if (a.top > 0)
-        asm volatile("st.shared::cluster.u64 [%0], %1;"
-                     ::"r"(first_cta(&s_best[rank][lane])), "l"(s_list[0][lane]) : "memory");
-      if (lane == 0) {
-        Sums t = s_sum[0];
-        for (int q = 1; q < kWarps; ++q) t.join(s_sum[q].m, s_sum[q].s, s_sum[q].u);
-        asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\t"
-                     "st.shared::cluster.f32 [%0 + 8], %3;"
-                     ::"r"(first_cta(&s_part[rank])), "f"(t.m), "f"(t.s), "f"(t.u) : "memory");
-      }
+__device__ __forceinline__ Key exchange(Key k, int j, bool larger) {
+  const Key q = __shfl_xor_sync(0xffffffffu, k, j);
+  return (q > k) == larger ? q : k;
+}
+
+// The alternatives where the candidates are too many (logits in falling order, or many equal ones): each warp keeps the
+// 32 largest in order, a list per warp at s.cand, which are then merged in pairs. Returns how many there are.
+template <int DT, int W>
+__device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, Key key, Key bound, Team<W>& s) {
+  const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5;
+  Key mine = 0ull;
+  revisit<DT, W>(row, j0, j1, key, bound, [&](Key q) {
+    unsigned int found = __ballot_sync(0xffffffffu, q > __shfl_sync(0xffffffffu, mine, 31));
+    while (found) {
+      const Key f = __shfl_sync(0xffffffffu, q, __ffs(found) - 1);
+      found &= found - 1;
+      const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
+      if (mine < f) mine = lane == 0 || above > f ? f : above;
     }
+  });
+  __syncwarp();
+  team_sync<W>();                            // the candidates' places are free
+  s.cand[warp * 32 + lane] = mine;
+  for (int n = W / 2; n > 0; n >>= 1) {
+    team_sync<W>();
+    if (warp < n) {
+      const Key q = s.cand[(warp + n) * 32 + 31 - lane];
+      mine = q > mine ? q : mine;
+#pragma unroll
+      for (int j = 16; j > 0; j >>= 1) mine = exchange(mine, j, (lane & j) == 0);
+    }
+    if (warp < n) s.cand[warp * 32 + lane] = mine;
+  }
+  const int have = __popc(__ballot_sync(0xffffffffu, mine != 0ull));
+  if (warp == 0 && lane == 0) s.n = have;
+  __syncwarp();
+  team_sync<W>();
+}
+
+// Of n candidates the a.top largest, each at its place: put(place, key).
+template <int W, class Put>
+__device__ __forceinline__ void place_top(const Key* cand, int n, int top, Put put) {
+  for (int i = threadIdx.x % (32 * W); i < n; i += 32 * W) {
+    const Key k = cand[i];
+    int above = 0;
+#pragma unroll 4
+    for (int q = 0; q < n; ++q) above += cand[q] > k;
+    if (above < top) put(above, k);
+  }
+}
+
+template <int DT, int W>
+__global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, int split) {
+  using P = Pieces<DT>;
+  constexpr int kTeam = 32 * W;
+  __shared__ Team<W> s_team[kWarps / W];
+  __shared__ Sums s_part[W == 1 ? 1 : kMaxCluster];
+  __shared__ Key s_best[W == 1 ? 1 : kMaxCluster * 32];
+  const mca_token_logprobs_args& a = p.a;
+  const int tid = threadIdx.x % kTeam, lane = tid & 31, warp = tid >> 5;
+  const int64_t r = W == 1 ? (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) : (int64_t)blockIdx.x / split;
+  if (W == 1 && r >= a.rows) return;
+  const int rank = W > 1 && split > 1 ? (int)cluster_rank() : 0;
+  Team<W>& s = s_team[W == 1 ? threadIdx.x >> 5 : 0];
+  const P row(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld, a.vocab);
+  const int j0 = W == 1 ? 0 : (int)((int64_t)row.count * rank / split);
+  const int j1 = W == 1 ? row.count : (int)((int64_t)row.count * (rank + 1) / split);
+  if (W > 1 && split > 1) cluster_arrive();                     // every CTA runs before one writes to another
+  if (tid == 0) s.n = 0;
+
+  // the pass: a piece at an end of the row that is not whole before or after the others of its thread
+  Seen<DT> seen;
+  {
+    int j = j0 + tid;
+    const int end = j1 == row.count && !row.whole(j1 - 1) ? j1 - 1 : j1;
+    if (j == 0 && !row.whole(0)) {
+      seen.take(row.part(0), 0);
+      j += kTeam;
+    }
+    const uint4* x = row.pieces() + j;
+    constexpr int kAhead = 4;
+    for (; j + (kAhead - 1) * kTeam < end; j += kAhead * kTeam, x += kAhead * kTeam) {
+      uint4 q[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) q[i] = x[i * kTeam];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) seen.take(q[i], j + i * kTeam);
+    }
+    for (; j < end; j += kTeam, x += kTeam) seen.take(*x, j);
+    if (j == end && end < j1) seen.take(row.part(end), end);
+  }
+  __syncwarp();
+  Sums t = team_sums<W>(seen.sums(), s);
+
+  // the candidates: logits that reach the bound
+  if (a.top > 0) {
+    Key key = 0ull;
+    if (seen.at >= 0) {
+      float v[P::N];
+      row.load(seen.at, v);
+#pragma unroll
+      for (int i = P::N - 1; i >= 0; --i)
+        if (v[i] == seen.top) key = order_key(seen.top, row.index(seen.at, i));
+    }
+    __syncwarp();
+    // k threads reach the smallest of the warps' k / W-th
+    Key bound = 0ull, rest = key;
+    for (int k = 0; k < (a.top + W - 1) / W; ++k) {
+      bound = group_max<32>(rest);
+      if (rest == bound) rest = 0ull;
+    }
+    if constexpr (W > 1) {
+      if (lane == 0) s.key[warp] = bound;
+      __syncthreads();
+      for (int q = 0; q < W; ++q) bound = s.key[q] < bound ? s.key[q] : bound;
+    }
+    __syncwarp();
+    revisit<DT, W>(row, j0, j1, key, bound, [&](Key q) {
+      if (q != 0ull) {
+        const int at = atomicAdd(&s.n, 1);
+        if (at < Team<W>::kCand) s.cand[at] = q;
+      }
+    });
+    __syncwarp();
+    team_sync<W>();
+    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row, j0, j1, key, bound, s);
+  }
+
+  const Key* cand = s.cand;
+  int n = a.top > 0 ? s.n : 0;
+  if (W > 1 && split > 1) {                                     // to the cluster's first CTA
+    if (a.top > 0) {
+      cluster_wait();
+      if (warp == 0 && lane >= n) {                             // no candidate for this place
+        asm volatile("st.shared::cluster.u64 [%0], %1;"
+                     ::"r"(first_cta(&s_best[rank * 32 + lane])), "l"(0ull) : "memory");
+      }
+      place_top<W>(cand, n, 32, [&](int at, Key k) {
+        asm volatile("st.shared::cluster.u64 [%0], %1;"
+                     ::"r"(first_cta(&s_best[rank * 32 + at])), "l"(k) : "memory");
+      });
+    } else {
+      cluster_wait();
+    }
+    if (tid == 0)
+      asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\t"
+                   "st.shared::cluster.f32 [%0 + 8], %3;"
+                   ::"r"(first_cta(&s_part[rank])), "f"(t.m), "f"(t.s), "f"(t.u) : "memory");
     cluster_arrive();
     cluster_wait();
     if (rank != 0) return;
-    if (a.top > 0) {
-      if (warp < split) s_list[warp][lane] = s_best[warp][lane];
-      merge_lists(s_list, split);
-    }
+    t = s_part[0];
+    for (int q = 1; q < split; ++q) t.join(s_part[q].m, s_part[q].s, s_part[q].u);
+    cand = s_best;
+    n = a.top > 0 ? split * 32 : 0;
   }
-  if (warp == 0) {
-    const Sums* const part = split > 1 ? s_part : s_sum;
-    Sums t = part[0];
-    for (int q = 1; q < (split > 1 ? split : kWarps); ++q) t.join(part[q].m, part[q].s, part[q].u);
-    if (lane == 0) write_row<DT>(p, r, row.x, t);
-    if (lane < a.top) write_top(a, r, lane, s_list[0][lane], Row(t));
+  const Row w(t);
+  int found = n;
+  if (W > 1 && split > 1 && a.top > 0) {                        // empty places of the lists
+    found = 0;
+    for (int q = 0; q < split; ++q) found += __popc(__ballot_sync(0xffffffffu, s_best[q * 32 + lane] != 0ull));
   }
+  if (t.m <= Range<DT>::high || (found < a.top && !w.bad)) {
+    __syncwarp();
+    team_sync<W>();
+    exact_row<DT, W>(p, r, s);
+    return;
+  }
+  if (tid == 0) write_row<DT>(p, r, row.x, t);
+  if (w.bad) {
+    if (tid < a.top) write_top(a, r, tid, 0ull, w);
+    return;
+  }
+  place_top<W>(cand, n, a.top, [&](int at, Key k) {
+    if (k != 0ull) write_top(a, r, at, k, w);
+  });
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -424,6 +630,14 @@ struct Grad {
   __device__ __forceinline__ float of(float x) const {
     const float lp = x - lse, e = ex2_ftz(lp * kLog2e);
     return none ? 0.0f : -e * fmaf(ge, fmaxf(lp, kNoTerm) + h, gl);
+  }
+  // The same for two logits, rows that are not none.
+  __device__ __forceinline__ float2 of(float2 x) const {
+    float2 lp = add2(x, make_float2(-lse, -lse));
+    const float2 p = mul2(lp, make_float2(kLog2e, kLog2e));
+    const float2 e = make_float2(-ex2_ftz(p.x), -ex2_ftz(p.y));
+    lp = add2(make_float2(fmaxf(lp.x, kNoTerm), fmaxf(lp.y, kNoTerm)), make_float2(h, h));
+    return mul2(e, fma2(make_float2(ge, ge), lp, make_float2(gl, gl)));
   }
 };
 
@@ -470,7 +684,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(mca_token_l
     else
       row.load(j, v);
 #pragma unroll
-    for (int k = 0; k < P::N; ++k) v[k] = g.of(v[k]);
+    for (int k = 0; k < P::N; k += 2) {
+      const float2 d = g.of(make_float2(v[k], v[k + 1]));
+      v[k] = g.none ? 0.0f : d.x;
+      v[k + 1] = g.none ? 0.0f : d.y;
+    }
     const int at = g.t - row.index(j, 0);
     if (at >= 0 && at < P::N && !g.none) {
 #pragma unroll
@@ -514,7 +732,12 @@ cudaError_t launch_logprobs_t(const LogprobArgs& p, cudaStream_t s) {
     else launch_small<DT, 32, 32>(p, s);
     return cudaGetLastError();
   }
-  // CTAs per row: while four CTAs per SM have no row of their own, 2048 logits each at least
+  // a warp per row where rows are many and short; else a CTA, or more while four CTAs per SM have no row of their
+  // own and 2048 logits each at least
+  if (V <= kTeamVocab || (V <= kWarpVocab && p.a.rows >= kWarpRows)) {
+    logprobs_kernel<DT, 1><<<(unsigned int)((p.a.rows + kWarps - 1) / kWarps), kThreads, 0, s>>>(p, 1);
+    return cudaGetLastError();
+  }
   int split = 1;
   while (split < kMaxCluster && p.a.rows * split * 2 <= 4 * 152 && V / (split * 2) >= 2048) split *= 2;
   cudaLaunchConfig_t cfg{};
@@ -528,7 +751,7 @@ cudaError_t launch_logprobs_t(const LogprobArgs& p, cudaStream_t s) {
   at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, logprobs_kernel<DT>, p, split);
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel<DT, kWarps>, p, split);
 }
 
 template <int DT, int L>

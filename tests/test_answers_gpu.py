@@ -272,7 +272,8 @@ def test_logprobs_sizes(gpu_lib, vocab, dtype):
 
 
 @pytest.mark.parametrize("rows,vocab,top", [(1, 128000, 20), (2, 160001, 32), (400, 3001, 8),
-                                            (1500, 700, 5), (5000, 65, 5), (20011, 10, 1), (9, 262144, 1)])
+                                            (1500, 700, 5), (5000, 65, 5), (20011, 10, 1), (9, 262144, 1),
+                                            (1100, 1500, 32), (1031, 8191, 20), (1030, 2049, 1)])
 def test_logprobs_many(gpu_lib, rows, vocab, top):
     rng = np.random.default_rng(rows)
     x = (2 * rng.standard_normal((rows, vocab))).astype(np.float32)
@@ -325,6 +326,25 @@ def test_alternatives_in_any_order(gpu_lib, vocab, top):
     for step in (8, 32, 256, 1024, 2048, 4096):
         rows.append(np.where(i % step == step // 2, 8.0 - i / vocab, 0.0))
     check_logprobs(gpu_lib, np.stack(rows), rng.integers(0, vocab, len(rows)), top, "float32")
+
+
+@pytest.mark.parametrize("vocab,top", [(1100, 32), (3000, 7), (8000, 32)])
+def test_many_rows_in_any_order(gpu_lib, vocab, top):
+    """The same rows, and rows whose mask leaves nothing or less than is asked for, among more than a thousand."""
+    i = np.arange(vocab)
+    rng = np.random.default_rng(vocab)
+    x = rng.standard_normal((1030, vocab))
+    x[0], x[1], x[2], x[3] = -i / 64.0, i / 64.0, 0.0, i % 2
+    x[4] = np.where(i % 32 == 16, 8.0 - i / vocab, 0.0)
+    x[5] = np.where(i % 256 == 128, 8.0, rng.integers(0, 3, vocab))
+    x[6] = -np.inf
+    x[7] = np.where(i < 5, 1.0, -np.inf)
+    x[8] = np.where(i >= vocab - 5, 1.0, np.finfo(np.float32).min)
+    x[9, vocab // 2] = np.nan
+    x[10, 0] = np.inf
+    x[11] = -1e32
+    x[1029] = -i / 64.0
+    check_logprobs(gpu_lib, x, rng.integers(0, vocab, 1030), top, "float32")
 
 
 def test_logprobs_of_shifted_rows(gpu_lib):
