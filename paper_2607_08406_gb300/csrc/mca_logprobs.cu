@@ -6,11 +6,10 @@
 // is scaled, so that a common shift of a row loses nothing. Both kernels read every logit once; the gradient is a
 // product per logit. What bounds them is the memory: 2048 x 50001 bf16, 0.2 GB, takes 30 us at 6.8 TB/s.
 //
-// Alternatives without a second pass: a thread remembers in which of its 16-byte pieces its largest logit was (one
-// comparison a piece). The threads' largest give a bound that the k-th alternative cannot be below, and not many
-// more than k threads reach it, so that only their pieces are read again (from L2). What is found there is few
-// enough to be put in order by counting. (Sorting the threads' largest and merging lists over the CTA took 9 us of a
-// row's 25.)
+// Alternatives without a second pass: a thread keeps the largest logit of each of up to 8 groups of its 16-byte pieces. The
+// threads' largest give a bound that the k-th alternative cannot be below; few more than k groups reach it, and only
+// these are read again (from L2). What is found there is few enough to be put in order by counting. (Sorting the
+// threads' largest and merging lists over the CTA took 9 us of a row's 25.)
 #include <algorithm>
 
 #include "mca_answers.h"
@@ -97,21 +96,25 @@ __device__ __forceinline__ void write_top(const mca_token_logprobs_args& a, int6
 // ------------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 128;
 constexpr int kSmallVocab = 1024;
+// Up to which the rounds of the small kernel find several alternatives faster, and rows below which its latency counts:
+// 20000 x 1000 bf16 with 8 takes 74 us in rounds and 34 otherwise, 20000 x 200 with 5 20 and 25, 100 x 500 4 and 6.
+constexpr int kRoundVocab = 256;
+constexpr int kRoundRows = 2048;
 
+// The largest of a value over the L lanes of a row.
 template <int L>
-__device__ __forceinline__ Key group_max(Key k) {
+__device__ __forceinline__ unsigned int lanes_max(unsigned int v) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(0xffffffffu, v);
+  } else {
 #pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) {
-    const Key q = __shfl_xor_sync(0xffffffffu, k, o);
-    k = q > k ? q : k;
+    for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
   }
-  return k;
 }
-template <>
-__device__ __forceinline__ Key group_max<32>(Key k) {
-  const unsigned int hi = __reduce_max_sync(0xffffffffu, (unsigned int)(k >> 32));
-  const unsigned int lo = __reduce_max_sync(0xffffffffu, (unsigned int)(k >> 32) == hi ? (unsigned int)k : 0u);
-  return (Key)hi << 32 | lo;
+__device__ __forceinline__ Key warp_max(Key k) {
+  const unsigned int hi = lanes_max<32>((unsigned int)(k >> 32));
+  return (Key)hi << 32 | lanes_max<32>((unsigned int)(k >> 32) == hi ? (unsigned int)k : 0u);
 }
 
 template <int DT, int L, int N>
@@ -142,17 +145,22 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
   if (live && t == 0) write_row<DT>(p, r, x, sum);
   if (a.top == 0) return;
   const Row w(sum);
-  Key last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {                     // the next in order, one round each
-    Key best = 0ull;
+  unsigned int u[N];                                    // the keys' upper halves; 0: none, or taken
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const Key q = order_key(z[i], t + L * i);
-      if (q < last && q > best) best = q;
-    }
-    best = group_max<L>(best);
-    if (live && t == 0) write_top(a, r, k, best, w);
-    last = best ? best : 1ull;
+  for (int i = 0; i < N; ++i) u[i] = (unsigned int)(order_key(z[i], 0) >> 32);
+  for (int k = 0; k < a.top; ++k) {                     // the next in order, one round each
+    unsigned int best = 0u, at = 0u;                    // and the complement of its index
+#pragma unroll
+    for (int i = 0; i < N; ++i) best = max(best, u[i]);
+    best = lanes_max<L>(best);
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i)
+      if (u[i] == best) at = ~(unsigned int)(t + L * i);
+    at = lanes_max<L>(at);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (~at == (unsigned int)(t + L * i)) u[i] = 0u;
+    if (live && t == 0) write_top(a, r, k, best ? (Key)best << 32 | at : 0ull, w);
   }
 }
 
@@ -162,9 +170,9 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary (a CTA's threads have no piece each),
-constexpr int kWarpVocab = 8192;          //   up to this one from
-constexpr int kWarpRows = 1024;           //   so many rows
+constexpr int kAhead = 6;                 // pieces that a thread has on their way
+constexpr int kGroups = 8;                // groups of a thread's pieces
+constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary
 
 // A row's 16-byte pieces: piece j holds the logits j N - head .. of the row (the first and the last in part).
 template <int DT>
@@ -297,7 +305,7 @@ struct Seen {
     s.y *= f;
     m = to;
   }
-  __device__ __forceinline__ void take(const uint4& q, int j) {
+  __device__ __forceinline__ float take(const uint4& q, int j) {
     float2 v[Pieces<DT>::N / 2];
     const float b = clamp_piece<DT>(q, v);
     if (b > top) {
@@ -312,6 +320,7 @@ struct Seen {
       s = add2(s, e);
       u = fma2(e, d, u);
     }
+    return b;
   }
   // The sums relative to the largest logit.
   __device__ __forceinline__ Sums sums() {
@@ -320,22 +329,22 @@ struct Seen {
   }
 };
 
-// A team of W warps has a row: a warp of a CTA's eight, or the CTA.
+// A CTA of W warps has a row (or, of kWarps, a part of one).
 template <int W>
 __device__ __forceinline__ void team_sync() {
-  if constexpr (W == 1)
-    __syncwarp();
-  else
-    __syncthreads();
+  __syncwarp();
+  if constexpr (W > 1) __syncthreads();
 }
 
 template <int W>
 struct Team {
-  static constexpr int kCand = W == 1 ? 64 : 512;
+  static constexpr int kCand = 64 * W;
   static_assert(kCand >= W * 32, "the lists of ordered_top");
   Sums sum[W];
   Key key[W];
-  int n;                                    // candidates
+  int n, flagged;                           // candidates; groups whose largest logit reaches the bound
+  unsigned short flag[kGroups * 32 * W];    // their threads and numbers
+  float top[kGroups][32 * W];               // largest logits of the threads' groups
   Key cand[kCand];
 };
 
@@ -348,7 +357,7 @@ __device__ __forceinline__ Sums team_sums(Sums t, Team<W>& s) {
   if constexpr (W > 1) {
     const int lane = threadIdx.x & 31;
     if (lane == 0) s.sum[threadIdx.x >> 5] = t;
-    __syncthreads();
+    team_sync<W>();
     t = s.sum[lane % W];
 #pragma unroll
     for (int o = W / 2; o > 0; o >>= 1)
@@ -367,7 +376,7 @@ template <int DT, int W>
 __device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>& s) {
   const mca_token_logprobs_args& a = p.a;
   const elem_t<DT>* x = static_cast<const elem_t<DT>*>(a.logits) + r * a.ld;
-  const int tid = threadIdx.x % (32 * W), lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Sums t{kLowest, 0.0f, 0.0f};
   for (int v = tid; v < a.vocab; v += 32 * W) t.m = fmaxf(t.m, elem_f32(x[v]));
   for (int v = tid; v < a.vocab; v += 32 * W) t.add(elem_f32(x[v]));
@@ -385,11 +394,11 @@ __device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>&
         if (q < last && q > best) best = q;
       }
     __syncwarp();
-    best = group_max<32>(best);
+    best = warp_max(best);
     if constexpr (W > 1) {
-      __syncthreads();
+      team_sync<W>();
       if (lane == 0) s.key[warp] = best;
-      __syncthreads();
+      team_sync<W>();
       for (int q = 0; q < W; ++q) best = s.key[q] > best ? s.key[q] : best;
     }
     if (tid == 0) write_top(a, r, k, best, w);
@@ -397,35 +406,39 @@ __device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>&
   }
 }
 
-// The pieces of the threads whose largest logit reaches the bound, again: visit(key) for each logit that does. The whole
-// warp takes a thread's pieces, one per lane.
-template <int DT, int W, class Visit>
-__device__ __forceinline__ void revisit(const Pieces<DT>& row, int j0, int j1, Key key, Key bound, Visit visit) {
-  constexpr int N = Pieces<DT>::N;
-  const int lane = threadIdx.x & 31, first = threadIdx.x % (32 * W) - lane;
+// The candidates: the logits that reach the bound, which lie in the groups whose largest does. Their pieces are read again
+// by the whole CTA, all at once. A thread's group g holds its pieces g size .. of the order that it took them in.
+template <int DT, int W>
+__device__ __forceinline__ void find_candidates(const Pieces<DT>& row, int j0, int j1, int size, float top, Key bound,
+                                                Team<W>& s) {
+  constexpr int N = Pieces<DT>::N, kTeam = 32 * W;
+  const int tid = threadIdx.x;
+  // (logits at or below the range's low: exact_row, if the row has no others)
   const float low = fmaxf(Range<DT>::low, bound ? key_value(bound) : -INFINITY);
-  unsigned int todo = __ballot_sync(0xffffffffu, key != 0ull && key >= bound);
-  while (todo) {
-    const int owner = __ffs(todo) - 1;
-    todo &= todo - 1;
-    for (int b = j0 + first + owner; b < j1; b += 32 * 32 * W) {
-      const int j = b + lane * 32 * W;
-      float v[N];
-      float m = -INFINITY;
-      if (j < j1) {
-        row.load(j, v);
+  if (top >= low && top > Range<DT>::low) {
+    for (int g = 0; j0 + g * size * kTeam + tid < j1; ++g)
+      if (s.top[g][tid] >= low) s.flag[atomicAdd(&s.flagged, 1)] = (unsigned short)(g * kTeam + tid);
+  }
+  __syncwarp();
+  team_sync<W>();
+  const int items = s.flagged * size;
+  for (int i = tid; i < items; i += kTeam) {
+    const int f = s.flag[i / size];
+    const int j = j0 + (f / kTeam * size + i % size) * kTeam + f % kTeam;
+    if (j >= j1) continue;
+    float v[N];
+    row.load(j, v);
+    float m = v[0];
 #pragma unroll
-        for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-      }
-      // (logits at or below the range's low: exact_row, if the row has no others)
-      const bool any = m >= low && m > Range<DT>::low;
-      if (__ballot_sync(0xffffffffu, any)) {
+    for (int k = 1; k < N; ++k) m = fmaxf(m, v[k]);
+    if (!(m >= low && m > Range<DT>::low)) continue;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const Key q = any && v[i] > Range<DT>::low ? order_key(v[i], row.index(j, i)) : 0ull;
-          visit(q != 0ull && q >= bound ? q : 0ull);
-        }
-      }
+    for (int k = 0; k < N; ++k) {
+      if (v[k] < low || !(v[k] > Range<DT>::low)) continue;
+      const Key c = order_key(v[k], row.index(j, k));
+      if (c < bound) continue;
+      const int slot = atomicAdd(&s.n, 1);
+      if (slot < Team<W>::kCand) s.cand[slot] = c;
     }
   }
 }
@@ -439,17 +452,35 @@ __device__ __forceinline__ Key exchange(Key k, int j, bool larger) {
 // 32 largest in order, a list per warp at s.cand, which are then merged in pairs. Returns how many there are.
 template <int DT, int W>
 __device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, Key key, Key bound, Team<W>& s) {
-  const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5;
+  constexpr int N = Pieces<DT>::N;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Key mine = 0ull;
-  revisit<DT, W>(row, j0, j1, key, bound, [&](Key q) {
-    unsigned int found = __ballot_sync(0xffffffffu, q > __shfl_sync(0xffffffffu, mine, 31));
-    while (found) {
-      const Key f = __shfl_sync(0xffffffffu, q, __ffs(found) - 1);
-      found &= found - 1;
-      const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
-      if (mine < f) mine = lane == 0 || above > f ? f : above;
+  // the warp takes its threads' pieces one thread after the other, a piece per lane
+  unsigned int todo = __ballot_sync(0xffffffffu, key != 0ull && key >= bound);
+  while (todo) {
+    const int owner = __ffs(todo) - 1;
+    todo &= todo - 1;
+    for (int b = j0 + warp * 32 + owner; b < j1; b += 32 * 32 * W) {
+      const int j = b + lane * 32 * W;
+      float v[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = -INFINITY;
+      if (j < j1) row.load(j, v);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const Key q = v[i] > Range<DT>::low ? order_key(v[i], row.index(j, i)) : 0ull;
+        const Key last = __shfl_sync(0xffffffffu, mine, 31);
+        unsigned int found = __ballot_sync(0xffffffffu, q > last && q >= bound);
+        while (found) {
+          const Key f = __shfl_sync(0xffffffffu, q, __ffs(found) - 1);
+          found &= found - 1;
+          const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
+          if (mine < f) mine = lane == 0 || above > f ? f : above;
+        }
+      }
     }
-  });
+  }
   __syncwarp();
   team_sync<W>();                            // the candidates' places are free
   s.cand[warp * 32 + lane] = mine;
@@ -472,7 +503,7 @@ __device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, 
 // Of n candidates the a.top largest, each at its place: put(place, key).
 template <int W, class Put>
 __device__ __forceinline__ void place_top(const Key* cand, int n, int top, Put put) {
-  for (int i = threadIdx.x % (32 * W); i < n; i += 32 * W) {
+  for (int i = threadIdx.x; i < n; i += 32 * W) {
     const Key k = cand[i];
     int above = 0;
 #pragma unroll 4
@@ -482,44 +513,64 @@ __device__ __forceinline__ void place_top(const Key* cand, int n, int top, Put p
 }
 
 template <int DT, int W>
-__global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, int split) {
+__global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(LogprobArgs p, int split) {
   using P = Pieces<DT>;
   constexpr int kTeam = 32 * W;
-  __shared__ Team<W> s_team[kWarps / W];
-  __shared__ Sums s_part[W == 1 ? 1 : kMaxCluster];
-  __shared__ Key s_best[W == 1 ? 1 : kMaxCluster * 32];
+  __shared__ Team<W> s;
+  __shared__ uint4 s_ring[kAhead][kTeam];
+  constexpr bool kWhole = W == kWarps;                          // a row may have a cluster's CTAs
+  __shared__ Sums s_part[kWhole ? kMaxCluster : 1];
+  __shared__ Key s_best[kWhole ? kMaxCluster * 32 : 1];
   const mca_token_logprobs_args& a = p.a;
-  const int tid = threadIdx.x % kTeam, lane = tid & 31, warp = tid >> 5;
-  const int64_t r = W == 1 ? (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) : (int64_t)blockIdx.x / split;
-  if (W == 1 && r >= a.rows) return;
-  const int rank = W > 1 && split > 1 ? (int)cluster_rank() : 0;
-  Team<W>& s = s_team[W == 1 ? threadIdx.x >> 5 : 0];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t r = kWhole ? (int64_t)blockIdx.x / split : (int64_t)blockIdx.x;
+  const int rank = kWhole && split > 1 ? (int)cluster_rank() : 0;
   const P row(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld, a.vocab);
-  const int j0 = W == 1 ? 0 : (int)((int64_t)row.count * rank / split);
-  const int j1 = W == 1 ? row.count : (int)((int64_t)row.count * (rank + 1) / split);
-  if (W > 1 && split > 1) cluster_arrive();                     // every CTA runs before one writes to another
-  if (tid == 0) s.n = 0;
+  const int j0 = kWhole ? (int)((int64_t)row.count * rank / split) : 0;
+  const int j1 = kWhole ? (int)((int64_t)row.count * (rank + 1) / split) : row.count;
+  if (kWhole && split > 1) cluster_arrive();                     // every CTA runs before one writes to another
+  if (tid == 0) s.n = s.flagged = 0;
 
-  // the pass: a piece at an end of the row that is not whole before or after the others of its thread
+  // the pass
   Seen<DT> seen;
+  const int size = ((j1 - j0 + kTeam - 1) / kTeam + kGroups - 1) / kGroups;     // of a group
   {
-    int j = j0 + tid;
-    const int end = j1 == row.count && !row.whole(j1 - 1) ? j1 - 1 : j1;
-    if (j == 0 && !row.whole(0)) {
-      seen.take(row.part(0), 0);
-      j += kTeam;
-    }
-    const uint4* x = row.pieces() + j;
-    constexpr int kAhead = 4;
-    for (; j + (kAhead - 1) * kTeam < end; j += kAhead * kTeam, x += kAhead * kTeam) {
-      uint4 q[kAhead];
+    // kAhead pieces on their way to shared memory, each to its thread's own places: no registers, no barriers. A piece at an
+    // end of the row that is not whole is put there by its thread.
+    const unsigned int ring = (unsigned int)__cvta_generic_to_shared(&s_ring[0][tid]);
+    int j = j0 + tid, slot = 0;
+    auto ask = [&](int at) {
+      if (at < j1) {
+        const unsigned int to = ring + (unsigned int)(slot * kTeam * 16);
+        if (row.whole(at)) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row.pieces() + at) : "memory");
+        } else {
+          const uint4 q = row.part(at);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                       ::"r"(to), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      slot = slot + 1 == kAhead ? 0 : slot + 1;
+    };
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) q[i] = x[i * kTeam];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) seen.take(q[i], j + i * kTeam);
+    for (int i = 0; i < kAhead; ++i) ask(j + i * kTeam);
+    float b = -INFINITY;                                        // the group's largest
+    int left = size, group = 0;
+    for (; j < j1; j += kTeam) {
+      uint4 q;
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+                   : "r"(ring + (unsigned int)(slot * kTeam * 16)) : "memory");
+      b = fmaxf(b, seen.take(q, j));
+      if (--left == 0 || j + kTeam >= j1) {
+        s.top[group++][tid] = b;
+        b = -INFINITY;
+        left = size;
+      }
+      ask(j + kAhead * kTeam);
     }
-    for (; j < end; j += kTeam, x += kTeam) seen.take(*x, j);
-    if (j == end && end < j1) seen.take(row.part(end), end);
   }
   __syncwarp();
   Sums t = team_sums<W>(seen.sums(), s);
@@ -538,21 +589,16 @@ __global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, in
     // k threads reach the smallest of the warps' k / W-th
     Key bound = 0ull, rest = key;
     for (int k = 0; k < (a.top + W - 1) / W; ++k) {
-      bound = group_max<32>(rest);
+      bound = warp_max(rest);
       if (rest == bound) rest = 0ull;
     }
     if constexpr (W > 1) {
       if (lane == 0) s.key[warp] = bound;
-      __syncthreads();
+      team_sync<W>();
       for (int q = 0; q < W; ++q) bound = s.key[q] < bound ? s.key[q] : bound;
     }
     __syncwarp();
-    revisit<DT, W>(row, j0, j1, key, bound, [&](Key q) {
-      if (q != 0ull) {
-        const int at = atomicAdd(&s.n, 1);
-        if (at < Team<W>::kCand) s.cand[at] = q;
-      }
-    });
+    find_candidates<DT, W>(row, j0, j1, size, seen.top, bound, s);
     __syncwarp();
     team_sync<W>();
     if (s.n > Team<W>::kCand) ordered_top<DT, W>(row, j0, j1, key, bound, s);
@@ -560,20 +606,15 @@ __global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, in
 
   const Key* cand = s.cand;
   int n = a.top > 0 ? s.n : 0;
-  if (W > 1 && split > 1) {                                     // to the cluster's first CTA
-    if (a.top > 0) {
-      cluster_wait();
-      if (warp == 0 && lane >= n) {                             // no candidate for this place
-        asm volatile("st.shared::cluster.u64 [%0], %1;"
-                     ::"r"(first_cta(&s_best[rank * 32 + lane])), "l"(0ull) : "memory");
-      }
-      place_top<W>(cand, n, 32, [&](int at, Key k) {
-        asm volatile("st.shared::cluster.u64 [%0], %1;"
-                     ::"r"(first_cta(&s_best[rank * 32 + at])), "l"(k) : "memory");
-      });
-    } else {
-      cluster_wait();
-    }
+  if (kWhole && split > 1) {                                    // to the cluster's first CTA
+    cluster_wait();
+    if (tid < a.top && tid >= n)                                // no candidate for this place
+      asm volatile("st.shared::cluster.u64 [%0], %1;"
+                   ::"r"(first_cta(&s_best[rank * a.top + tid])), "l"(0ull) : "memory");
+    place_top<W>(cand, n, a.top, [&](int at, Key k) {
+      asm volatile("st.shared::cluster.u64 [%0], %1;"
+                   ::"r"(first_cta(&s_best[rank * a.top + at])), "l"(k) : "memory");
+    });
     if (tid == 0)
       asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\t"
                    "st.shared::cluster.f32 [%0 + 8], %3;"
@@ -584,13 +625,13 @@ __global__ void __launch_bounds__(kThreads, 6) logprobs_kernel(LogprobArgs p, in
     t = s_part[0];
     for (int q = 1; q < split; ++q) t.join(s_part[q].m, s_part[q].s, s_part[q].u);
     cand = s_best;
-    n = a.top > 0 ? split * 32 : 0;
+    n = split * a.top;
   }
   const Row w(t);
   int found = n;
-  if (W > 1 && split > 1 && a.top > 0) {                        // empty places of the lists
+  if (kWhole && split > 1 && a.top > 0) {                        // empty places of the lists
     found = 0;
-    for (int q = 0; q < split; ++q) found += __popc(__ballot_sync(0xffffffffu, s_best[q * 32 + lane] != 0ull));
+    for (int q = 0; q < n; q += 32) found += __popc(__ballot_sync(0xffffffffu, q + lane < n && s_best[q + lane] != 0ull));
   }
   if (t.m <= Range<DT>::high || (found < a.top && !w.bad)) {
     __syncwarp();
@@ -719,10 +760,16 @@ void launch_small(const LogprobArgs& p, cudaStream_t s) {
   logprobs_small_kernel<DT, L, N><<<(unsigned int)((p.a.rows + kPer - 1) / kPer), kSmallThreads, 0, s>>>(p);
 }
 
+template <int DT, int W>
+cudaError_t launch_team(const LogprobArgs& p, cudaStream_t s) {
+  logprobs_kernel<DT, W><<<(unsigned int)p.a.rows, 32 * W, 0, s>>>(p, 1);
+  return cudaGetLastError();
+}
+
 template <int DT>
 cudaError_t launch_logprobs_t(const LogprobArgs& p, cudaStream_t s) {
   const int V = p.a.vocab;
-  if (V <= kSmallVocab) {
+  if (V <= kRoundVocab || (V <= kSmallVocab && (p.a.top <= 1 || p.a.rows < kRoundRows))) {
     if (V <= 16) launch_small<DT, 4, 4>(p, s);
     else if (V <= 32) launch_small<DT, 8, 4>(p, s);
     else if (V <= 64) launch_small<DT, 16, 4>(p, s);
@@ -732,14 +779,15 @@ cudaError_t launch_logprobs_t(const LogprobArgs& p, cudaStream_t s) {
     else launch_small<DT, 32, 32>(p, s);
     return cudaGetLastError();
   }
-  // a warp per row where rows are many and short; else a CTA, or more while four CTAs per SM have no row of their
-  // own and 2048 logits each at least
-  if (V <= kTeamVocab || (V <= kWarpVocab && p.a.rows >= kWarpRows)) {
-    logprobs_kernel<DT, 1><<<(unsigned int)((p.a.rows + kWarps - 1) / kWarps), kThreads, 0, s>>>(p, 1);
-    return cudaGetLastError();
-  }
+  // Warps per row: as many as run at once, so that all rows do; one for short rows (a CTA's threads would have no piece
+  // each). 2048 x 50001 bf16 takes 36 us with two, 48 with eight in more than two waves.
+  const int64_t warps = 32 * 152 / p.a.rows;
+  if (V <= kTeamVocab || warps < 2) return launch_team<DT, 1>(p, s);
+  if (warps < 4) return launch_team<DT, 2>(p, s);
+  if (warps < 8) return launch_team<DT, 4>(p, s);
+  // or CTAs of a cluster, while SMs have no row of their own and 2048 logits each at least
   int split = 1;
-  while (split < kMaxCluster && p.a.rows * split * 2 <= 4 * 152 && V / (split * 2) >= 2048) split *= 2;
+  while (split < kMaxCluster && p.a.rows * split * 2 <= 152 && V / (split * 2) >= 2048) split *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned int)(p.a.rows * split));
   cfg.blockDim = dim3(kThreads);

@@ -435,9 +435,10 @@ def _cuda(name, t, dtypes, device=None, ndim=1):
         raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
     if device is not None and t.device != device:
         raise ValueError(f"{name}: on {t.device}, expected {device}")
-    if t.dim() != ndim:
-        raise ValueError(f"{name}: {t.dim()} dimensions, expected {ndim}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    shape = t.shape
+    if len(shape) != ndim:
+        raise ValueError(f"{name}: {len(shape)} dimensions, expected {ndim}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: stride {t.stride(-1)} between elements of a row, expected 1")
 
 
@@ -455,40 +456,37 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+_dtypes: dict = {}      # torch dtype -> mca_dtype
+
+
 def _float_types():
-    import torch
-    return torch.float32, torch.float16, torch.bfloat16
+    if not _dtypes:
+        import torch
+        _dtypes.update({getattr(torch, n): c for n, c in DTYPE.items()})
+    return _dtypes
 
 
 def _dtype_code(dtype) -> int:
     try:
-        return DTYPE[str(dtype).split(".")[-1]]
+        return _float_types()[dtype]
     except KeyError:
         raise ValueError(f"dtype {dtype}: expected float32, float16 or bfloat16") from None
-
-
-@contextmanager
-def _other(device, stream):
-    """The device and stream that are not the current ones, for allocations and launches."""
-    import torch
-    with torch.cuda.device(device):
-        if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
-            yield
-        else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if stream
-                                   else torch.cuda.default_stream(device)):
-                yield
 
 
 def _on(device, stream, call):
     """call(stream's cudaStream_t) with the device current and tensors allocated on the stream."""
     import torch
-    if torch.cuda.current_device() == device.index:
-        cur = torch.cuda.current_stream().cuda_stream
+    index = device.index
+    if torch._C._cuda_getDevice() == index:
+        cur = torch._C._cuda_getCurrentRawStream(index)
         if stream is None or stream == cur:
             return call(cur)
-    with _other(device, stream):
-        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        if stream is None or stream == torch.cuda.current_stream().cuda_stream:
+            return call(torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if stream
+                               else torch.cuda.default_stream(device)):
+            return call(stream)
 
 
 def mca_quantize_rows(x, codes=None, scale=None, stream=None):
@@ -506,8 +504,8 @@ def mca_quantize_rows(x, codes=None, scale=None, stream=None):
     _vector("scale", scale, rows, torch.float32, dev)
 
     def call(s):
-        c = codes if codes is not None else torch.empty(
-            (rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=dev)[:, :cols]
+        c = codes if codes is not None else torch.empty_strided(
+            (rows, cols), ((cols + 15) // 16 * 16, 1), dtype=torch.int8, device=dev)
         sc = scale if scale is not None else torch.empty(rows, dtype=torch.float32, device=dev)
         _check(load_library().mca_quantize_rows(x.data_ptr(), _dtype_code(x.dtype), rows, cols,
                                                 _ld(x), c.data_ptr(), _ld(c), sc.data_ptr(), s))
