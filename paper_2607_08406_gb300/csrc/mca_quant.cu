@@ -1,23 +1,26 @@
 // Rows in 8-bit codes with a scale each (mca_quantize_rows): scale = max |x| / 127, code = x / scale to the nearest
 // integer. One read of x and one write of the codes bound it (2 + 1 bytes per bf16 element); a row's elements
-// wait in registers between the two steps, a warp per row up to kWarpCols columns and a CTA per row beyond. Rows
-// longer than a CTA's registers are read a second time, mostly from L2.
+// wait in registers between the two steps: 8 lanes have a row up to 256 columns, a warp up to 1024, a CTA up to 32768.
+// Longer rows are read a second time, mostly from L2. An element's quotient is a product with 1 / scale, rounded by an
+// addition, seven instructions with its place in the output; the pieces with one next to a half (one of 600) are
+// looked at again.
 #include "mca_answers.h"
+#include "mca_device.cuh"
 #include "mca_elem.cuh"
 
 namespace mca {
 
 namespace {
 
-constexpr int kWarpCols = 1024;    // columns up to which a warp holds a row (32 elements a lane)
-constexpr int kRowThreads = 256;   // a CTA's threads
-constexpr int kLaneElems = 32;     // elements that a thread holds
+constexpr int kRowThreads = 256;   // a CTA's threads, of short rows
 constexpr int kLongThreads = 1024; // threads of a CTA whose row does not fit in registers
 
-// x / s for |x| / s <= 127.5 to the nearest integer, halves to the even one. The product with 1 / s is off
-// by less than 127 * 3 * 2^-24 = 2.3e-5; where that might cross a half, the sign of |x| - (f + 1/2) s decides,
-// whose product is exact in an fma (8 + 24 bits) and whose difference rounds once, which keeps its sign (s is no
-// subnormal number: see row_scale).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 struct RowScale {
   float s, inv, up;                // scale and its inverse for elements multiplied by up
 };
@@ -28,7 +31,11 @@ __device__ __forceinline__ RowScale row_scale(float s) {
   return {s * up, 1.0f / (s * up), up};
 }
 
-__device__ __forceinline__ int code_of(float x, const RowScale& r) {
+// x / s for |x| / s <= 127.5 to the nearest integer, halves to the even one. The product with 1 / s is off
+// by less than 127 * 3 * 2^-24 = 2.3e-5; where that might cross a half, the sign of |x| - (f + 1/2) s decides,
+// whose product is exact in an fma (8 + 24 bits) and whose difference rounds once, which keeps its sign (s is no
+// subnormal number: see row_scale).
+__device__ __forceinline__ int exact_code(float x, const RowScale& r) {
   const float a = fabsf(x) * r.up;
   const float t = a * r.inv;
   float c = near_f32(t);
@@ -60,27 +67,63 @@ struct Pack {
 #pragma unroll
     for (int q = 0; q < N; ++q) e[q] = c + q < cols ? x[c + q] : elem_of<DT>(0.0f);
   }
-  // Largest magnitude so far; an infinity or NaN makes it infinite.
+  // The largest magnitude, of those here and t; NaN if one is.
   __device__ __forceinline__ float top(float t) const {
+    if constexpr (WIDE && DT != MCA_DTYPE_FP32) {
+      unsigned int m[4] = {u.x & 0x7fff7fffu, u.y & 0x7fff7fffu, u.z & 0x7fff7fffu, u.w & 0x7fff7fffu};
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-      const float v = fabsf(elem_f32(e[q]));
-      t = v <= 3.4028235e38f ? fmaxf(t, v) : INFINITY;
+      for (int k = 2; k > 0; k >>= 1)
+#pragma unroll
+        for (int q = 0; q < k; ++q) {
+          if constexpr (DT == MCA_DTYPE_BF16)
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(m[q]), "r"(m[q + k]));
+          else
+            asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(m[q]), "r"(m[q + k]));
+        }
+      const elem_t<DT>* h = reinterpret_cast<const elem_t<DT>*>(&m[0]);
+      return max_nan(t, max_nan(elem_f32(h[0]), elem_f32(h[1])));
+    } else {
+#pragma unroll
+      for (int q = 0; q < N; ++q) t = max_nan(t, fabsf(elem_f32(e[q])));
+      return t;
     }
-    return t;
   }
   __device__ __forceinline__ void store(int8_t* codes, int64_t c, int64_t cols, const RowScale& r,
                                         bool live) const {
-    int v[N];
+    // a code's bits are the lowest byte of its sum with kRound
+    unsigned int v[N];
+    float off = 0.0f;
+    if constexpr (WIDE) {
+      const float2 inv = make_float2(r.inv, r.inv), up = make_float2(kRound, kRound),
+                   down = make_float2(-kRound, -kRound), neg = make_float2(-1.0f, -1.0f);
 #pragma unroll
-    for (int q = 0; q < N; ++q) v[q] = live ? code_of(elem_f32(e[q]), r) : 0;
+      for (int q = 0; q < N; q += 2) {
+        const float2 t = mul2(make_float2(elem_f32(e[q]), elem_f32(e[q + 1])), inv), c = add2(t, up);
+        const float2 d = fma2(add2(c, down), neg, t);
+        off = fmaxf(off, fmaxf(fabsf(d.x), fabsf(d.y)));
+        v[q] = __float_as_uint(c.x);
+        v[q + 1] = __float_as_uint(c.y);
+      }
+    } else {
+      const float t = elem_f32(e[0]) * r.inv, c = __fadd_rn(t, kRound);
+      off = fabsf(t - __fsub_rn(c, kRound));
+      v[0] = __float_as_uint(c);
+    }
+    if (off > 0.4999f || r.up != 1.0f) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) v[q] = (unsigned int)exact_code(elem_f32(e[q]), r);
+    }
+    if (!live) {
+#pragma unroll
+      for (int q = 0; q < N; ++q) v[q] = 0u;
+    }
     if constexpr (WIDE) {
       if (c + N <= cols) {
         unsigned int w[N / 4];
 #pragma unroll
         for (int q = 0; q < N / 4; ++q)
-          w[q] = (v[4 * q] & 0xff) | (v[4 * q + 1] & 0xff) << 8 | (v[4 * q + 2] & 0xff) << 16 |
-                 (unsigned int)v[4 * q + 3] << 24;
+          w[q] = __byte_perm(__byte_perm(v[4 * q], v[4 * q + 1], 0x0040),
+                             __byte_perm(v[4 * q + 2], v[4 * q + 3], 0x0040), 0x5410);
         if constexpr (N == 8)
           *reinterpret_cast<uint2*>(codes + c) = make_uint2(w[0], w[1]);
         else
@@ -90,7 +133,7 @@ struct Pack {
     }
 #pragma unroll
     for (int q = 0; q < N; ++q)
-      if (c + q < cols) codes[c + q] = (int8_t)v[q];
+      if (c + q < cols) codes[c + q] = (int8_t)(v[q] & 0xffu);
   }
 };
 
@@ -98,30 +141,28 @@ struct Pack {
 template <int TPR>
 __device__ __forceinline__ float row_top(float t) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, o));
   if constexpr (TPR > 32) {
     __shared__ float s_red[TPR / 32];
     if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = t;
     __syncthreads();
     t = s_red[threadIdx.x & (TPR / 32 - 1)];
 #pragma unroll
-    for (int o = TPR / 64; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+    for (int o = TPR / 64; o > 0; o >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, o));
   }
   return t;
 }
 
-// TPR threads per row, which hold its elements; at most TPR * kLaneElems columns.
-template <int DT, bool WIDE, int TPR>
-__global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const void* __restrict__ xv,
-                                                                    int64_t rows, int cols,
-                                                                    int64_t ldx,
-                                                                    int8_t* __restrict__ codes,
-                                                                    int64_t ldc,
-                                                                    float* __restrict__ scale) {
+// TPR threads per row, which hold its elements, E each: at most TPR * E columns.
+template <int DT, bool WIDE, int TPR, int E>
+__global__ void __launch_bounds__(TPR > kRowThreads ? TPR : kRowThreads) quantize_rows_kernel(
+    const void* __restrict__ xv, int64_t rows, int cols, int64_t ldx, int8_t* __restrict__ codes, int64_t ldc,
+    float* __restrict__ scale) {
   using P = Pack<DT, WIDE>;
-  constexpr int NP = kLaneElems / P::N;
-  const int64_t r = (int64_t)blockIdx.x * (kRowThreads / TPR) + threadIdx.x / TPR;
-  if (r >= rows) return;             // whole warps: TPR is a multiple of 32
+  constexpr int NP = E / P::N, kPer = TPR > kRowThreads ? 1 : kRowThreads / TPR;
+  const int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR;
+  const bool there = row < rows;               // threads behind the last row take part in shuffles
+  const int64_t r = there ? row : rows - 1;
   const int t = threadIdx.x % TPR;
   const elem_t<DT>* x = static_cast<const elem_t<DT>*>(xv) + r * ldx;
   P p[NP];
@@ -133,6 +174,7 @@ __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const void* 
   for (int i = 0; i < NP; ++i)
     if (i * TPR * P::N < cols) top = p[i].top(top);
   top = row_top<TPR>(top);
+  if (!there) return;
   const float s = top < INFINITY ? top / 127.0f : NAN;
   if (t == 0) scale[r] = s;
   const RowScale rs = row_scale(s);
@@ -172,16 +214,27 @@ __global__ void fill_kernel(float* p, int64_t n, float v) {
   if (i < n) p[i] = v;
 }
 
+template <int DT, bool WIDE, int TPR, int E>
+void launch_rows_t(const void* x, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes, int64_t ldc,
+                   float* scale, cudaStream_t s) {
+  constexpr int kThreads = TPR > kRowThreads ? TPR : kRowThreads, kPer = kThreads / TPR;
+  quantize_rows_kernel<DT, WIDE, TPR, E><<<(unsigned int)((rows + kPer - 1) / kPer), kThreads, 0, s>>>(
+      x, rows, (int)cols, ldx, codes, ldc, scale);
+}
+
 template <int DT, bool WIDE>
 void launch_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes, int64_t ldc,
                  float* scale, cudaStream_t s) {
-  constexpr int kPer = kRowThreads / 32;
-  if (cols <= kWarpCols)
-    quantize_rows_kernel<DT, WIDE, 32><<<(unsigned int)((rows + kPer - 1) / kPer), kRowThreads, 0, s>>>(
-        x, rows, (int)cols, ldx, codes, ldc, scale);
-  else if (cols <= kRowThreads * kLaneElems)
-    quantize_rows_kernel<DT, WIDE, kRowThreads><<<(unsigned int)rows, kRowThreads, 0, s>>>(
-        x, rows, (int)cols, ldx, codes, ldc, scale);
+  if (cols <= 8 * 32)
+    launch_rows_t<DT, WIDE, 8, 32>(x, rows, cols, ldx, codes, ldc, scale, s);
+  else if (cols <= 32 * 32)
+    launch_rows_t<DT, WIDE, 32, 32>(x, rows, cols, ldx, codes, ldc, scale, s);
+  else if (cols <= 256 * 32)
+    launch_rows_t<DT, WIDE, 256, 32>(x, rows, cols, ldx, codes, ldc, scale, s);
+  else if (cols <= 512 * 32)
+    launch_rows_t<DT, WIDE, 512, 32>(x, rows, cols, ldx, codes, ldc, scale, s);
+  else if (cols <= 1024 * 32)
+    launch_rows_t<DT, WIDE, 1024, 32>(x, rows, cols, ldx, codes, ldc, scale, s);
   else
     quantize_long_rows_kernel<DT, WIDE><<<(unsigned int)rows, kLongThreads, 0, s>>>(
         x, cols, ldx, codes, ldc, scale);

@@ -426,66 +426,77 @@ def mca_selftest_wait_timeout():
 # the device's current torch stream), and tensors made here belong to it.
 # ------------------------------------------------------------------------------------------------
 
-def _cuda(name, t, dtypes, device=None, ndim=1):
-    """Checks a tensor argument."""
-    import torch
+torch = None             # the module, once one of the calls below has needed it
+_dtypes: dict = {}       # torch dtype -> mca_dtype
+_fn: dict = {}           # entry points by name
+
+
+def _ready():
+    """torch and the library, looked up once: a call's marshalling is what a small call costs."""
+    global torch
+    if not _fn:
+        import torch as t
+        lib = load_library()
+        torch = t
+        _dtypes.update({getattr(t, n): c for n, c in DTYPE.items()})
+        _fn.update({n: getattr(lib, n) for n in SIGNATURES})
+
+
+def _refuse(name, t, dtypes, device, ndim):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: not a CUDA tensor")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name}: on {t.device}, expected {device}")
-    shape = t.shape
-    if len(shape) != ndim:
-        raise ValueError(f"{name}: {len(shape)} dimensions, expected {ndim}")
-    if shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: stride {t.stride(-1)} between elements of a row, expected 1")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected device {device}")
+    if t.dim() != ndim:
+        raise ValueError(f"{name}: {t.dim()} dimensions, expected {ndim}")
+    raise ValueError(f"{name}: stride {t.stride(-1)} between elements of a row, expected 1")
+
+
+def _matrix(name, t, dtypes, device=None):
+    """Checks a matrix argument: (rows, columns, distance of rows)."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.dim() == 2:
+        d = t.get_device()
+        if d >= 0 and (device is None or d == device):
+            rows, cols = t.shape
+            ld, unit = t.stride()
+            if unit == 1 or cols <= 1:
+                return rows, cols, ld if rows > 1 else cols
+    _refuse(name, t, dtypes, device, 2)
 
 
 def _vector(name, t, n, dtype, device):
     """Address of a vector argument of n elements (None: NULL)."""
     if t is None:
         return None
-    _cuda(name, t, (dtype,), device)
-    if t.shape[0] != n:
-        raise ValueError(f"{name}: {t.shape[0]} elements, expected {n}")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device
+            and t.dim() == 1 and (n <= 1 or t.stride(0) == 1 or t.numel() <= 1)):
+        _refuse(name, t, (dtype,), device, 1)
+    if t.numel() != n:
+        raise ValueError(f"{name}: {t.numel()} elements, expected {n}")
     return t.data_ptr()
 
 
-def _ld(t):
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-_dtypes: dict = {}      # torch dtype -> mca_dtype
-
-
-def _float_types():
-    if not _dtypes:
-        import torch
-        _dtypes.update({getattr(torch, n): c for n, c in DTYPE.items()})
-    return _dtypes
-
-
 def _dtype_code(dtype) -> int:
+    _ready()
     try:
-        return _float_types()[dtype]
+        return _dtypes[dtype]
     except KeyError:
         raise ValueError(f"dtype {dtype}: expected float32, float16 or bfloat16") from None
 
 
-def _on(device, stream, call):
-    """call(stream's cudaStream_t) with the device current and tensors allocated on the stream."""
-    import torch
-    index = device.index
+def _on(index, stream, call):
+    """call(stream's cudaStream_t) with device `index` current and tensors allocated on the stream."""
     if torch._C._cuda_getDevice() == index:
         cur = torch._C._cuda_getCurrentRawStream(index)
         if stream is None or stream == cur:
             return call(cur)
-    with torch.cuda.device(device):
+    with torch.cuda.device(index):
         if stream is None or stream == torch.cuda.current_stream().cuda_stream:
             return call(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if stream
-                               else torch.cuda.default_stream(device)):
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream
+                               else torch.cuda.default_stream()):
             return call(stream)
 
 
@@ -493,42 +504,45 @@ def mca_quantize_rows(x, codes=None, scale=None, stream=None):
     """Rows of x [rows, cols] in 8 bits: (codes [rows, cols] int8, scale [rows] float32), x ~ scale *
     codes. New codes' rows start on 16-byte boundaries (a view of a wider matrix when cols is not a
     multiple of 16)."""
-    import torch
-    _cuda("x", x, _float_types(), ndim=2)
-    rows, cols = x.shape
-    dev = x.device
+    _ready()
+    rows, cols, ldx = _matrix("x", x, _dtypes)
+    dev = x.get_device()
     if codes is not None:
-        _cuda("codes", codes, (torch.int8,), dev, 2)
-        if codes.shape != x.shape:
+        crows, ccols, ldc = _matrix("codes", codes, (torch.int8,), dev)
+        if crows != rows or ccols != cols:
             raise ValueError(f"codes: shape {tuple(codes.shape)}, expected {tuple(x.shape)}")
-    _vector("scale", scale, rows, torch.float32, dev)
+    if scale is not None:
+        _vector("scale", scale, rows, torch.float32, dev)
 
     def call(s):
-        c = codes if codes is not None else torch.empty_strided(
-            (rows, cols), ((cols + 15) // 16 * 16, 1), dtype=torch.int8, device=dev)
-        sc = scale if scale is not None else torch.empty(rows, dtype=torch.float32, device=dev)
-        _check(load_library().mca_quantize_rows(x.data_ptr(), _dtype_code(x.dtype), rows, cols,
-                                                _ld(x), c.data_ptr(), _ld(c), sc.data_ptr(), s))
+        c, ld, sc = codes, 0, scale
+        if c is None:
+            ld = (cols + 15) // 16 * 16
+            c = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.int8, device=x.device)
+        else:
+            ld = ldc
+        if sc is None:
+            sc = torch.empty(rows, dtype=torch.float32, device=x.device)
+        _check(_fn["mca_quantize_rows"](x.data_ptr(), _dtypes[x.dtype], rows, cols, ldx,
+                                        c.data_ptr(), ld, sc.data_ptr(), s))
         return c, sc
 
     return _on(dev, stream, call)
 
 
 def _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype):
-    import torch
-    _cuda("x_codes", x_codes, (torch.int8,), ndim=2)
-    dev = x_codes.device
-    _cuda("w_codes", w_codes, (torch.int8,), dev, 2)
-    rows, n_in = x_codes.shape
-    n_out = w_codes.shape[0]
-    if w_codes.shape[1] != n_in:
-        raise ValueError(f"w_codes: {w_codes.shape[1]} columns, x_codes has {n_in}")
+    _ready()
+    i8, f32 = (torch.int8,), torch.float32
+    rows, n_in, ldx = _matrix("x_codes", x_codes, i8)
+    dev = x_codes.get_device()
+    n_out, w_in, ldw = _matrix("w_codes", w_codes, i8, dev)
+    if w_in != n_in:
+        raise ValueError(f"w_codes: {w_in} columns, x_codes has {n_in}")
     return mca_code_linear_args(
-        rows, n_in, n_out, x_codes.data_ptr(), _ld(x_codes),
-        _vector("x_scale", x_scale, rows, torch.float32, dev), w_codes.data_ptr(), _ld(w_codes),
-        _vector("w_scale", w_scale, n_out, torch.float32, dev),
-        _vector("bias", bias, n_out, torch.float32, dev), None, n_out,
-        0 if dtype is None else _dtype_code(dtype), ACT[act], float(act_param), None, 0, None)
+        rows, n_in, n_out, x_codes.data_ptr(), ldx, _vector("x_scale", x_scale, rows, f32, dev),
+        w_codes.data_ptr(), ldw, _vector("w_scale", w_scale, n_out, f32, dev),
+        _vector("bias", bias, n_out, f32, dev), None, n_out,
+        0 if dtype is None else _dtype_code(dtype), ACT[act], act_param)
 
 
 def mca_code_linear_workspace_size(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity",
@@ -536,7 +550,7 @@ def mca_code_linear_workspace_size(x_codes, x_scale, w_codes, w_scale, bias=None
     """Bytes of workspace of mca_code_linear for these operands."""
     a = _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype)
     n = c_size_t(0)
-    _check(load_library().mca_code_linear_workspace_size(ctypes.byref(a), ctypes.byref(n)))
+    _check(_fn["mca_code_linear_workspace_size"](ctypes.byref(a), ctypes.byref(n)))
     return n.value
 
 
@@ -545,33 +559,36 @@ def mca_code_linear(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity
     """act((x_codes w_codes^T) * x_scale[:, None] * w_scale + bias), sums exact: [rows, n_out] of
     `dtype` (default: out's, or float32). workspace: a uint8 CUDA tensor of at least
     mca_code_linear_workspace_size bytes on a 256-byte boundary (default: allocated for the call)."""
-    import torch
+    _ready()
     if out is not None:
-        _cuda("out", out, _float_types(), x_codes.device, 2)
         if dtype is not None and dtype != out.dtype:
             raise ValueError(f"out: dtype {out.dtype}, expected {dtype}")
         dtype = out.dtype
     a = _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype)
-    dev = x_codes.device
-    if out is not None and tuple(out.shape) != (a.rows, a.n_out):
-        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(a.rows, a.n_out)}")
+    dev = x_codes.get_device()
+    if out is not None:
+        rows, n_out, a.ldy = _matrix("out", out, _dtypes, dev)
+        if rows != a.rows or n_out != a.n_out:
+            raise ValueError(f"out: shape {tuple(out.shape)}, expected {(a.rows, a.n_out)}")
     if workspace is not None:
-        _cuda("workspace", workspace, (torch.uint8,), dev)
-    lib = load_library()
+        _vector("workspace", workspace, workspace.numel(), torch.uint8, dev)
+        if workspace.numel():
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    ref = ctypes.byref(a)
 
     def call(s):
-        y = out if out is not None else torch.empty((a.rows, a.n_out),
-                                                    dtype=dtype or torch.float32, device=dev)
-        ws = workspace
-        if ws is None:
+        y = out if out is not None else torch.empty(
+            (a.rows, a.n_out), dtype=dtype or torch.float32, device=x_codes.device)
+        a.y, a.stream = y.data_ptr(), s
+        status = _fn["mca_code_linear"](ref)
+        if status == MCA_ERR_OOM and workspace is None:      # it wants workspace
             n = c_size_t(0)
-            _check(lib.mca_code_linear_workspace_size(ctypes.byref(a), ctypes.byref(n)))
-            if n.value:
-                ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
-        if ws is not None and ws.numel():
-            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        a.y, a.ldy, a.stream = y.data_ptr(), _ld(y), s
-        _check(lib.mca_code_linear(ctypes.byref(a)))
+            _check(_fn["mca_code_linear_workspace_size"](ref, ctypes.byref(n)))
+            ws = torch.empty(n.value, dtype=torch.uint8, device=x_codes.device)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), n.value
+            status = _fn["mca_code_linear"](ref)
+        if status:
+            _check(status)
         return y
 
     return _on(dev, stream, call)
@@ -587,13 +604,14 @@ class TokenLogprobs(NamedTuple):
 
 
 def _logprob_outputs(rows, top, targets, dev):
-    import torch
-
-    def new(*shape):
-        return torch.empty(shape, dtype=torch.float32, device=dev)
-    return TokenLogprobs(new(rows) if targets else None, new(rows), new(rows),
-                         new(rows, top) if top else None,
-                         torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None)
+    f32 = torch.float32
+    logprob = torch.empty(rows, dtype=f32, device=dev) if targets else None
+    entropy = torch.empty(rows, dtype=f32, device=dev)
+    lse = torch.empty(rows, dtype=f32, device=dev)
+    if not top:
+        return TokenLogprobs(logprob, entropy, lse, None, None)
+    return TokenLogprobs(logprob, entropy, lse, torch.empty((rows, top), dtype=f32, device=dev),
+                         torch.empty((rows, top), dtype=torch.int32, device=dev))
 
 
 def _addr(t):
@@ -603,21 +621,20 @@ def _addr(t):
 def mca_token_logprobs(logits, targets=None, top: int = 0, stream=None) -> TokenLogprobs:
     """Log probabilities of targets [rows] (int32, -1: none) under softmax of each row of logits [rows,
     vocab], entropies, log-sum-exps and the `top` most probable symbols (at most 32)."""
-    import torch
-    _cuda("logits", logits, _float_types(), ndim=2)
-    rows, vocab = logits.shape
-    dev = logits.device
+    _ready()
+    rows, vocab, ld = _matrix("logits", logits, _dtypes)
+    dev = logits.get_device()
     t = _vector("targets", targets, rows, torch.int32, dev)
     if not 0 <= top <= MAX_TOP:
         raise ValueError(f"top = {top} outside 0..{MAX_TOP}")
 
     def call(s):
-        r = _logprob_outputs(rows, top, targets is not None, dev)
+        r = _logprob_outputs(rows, top, t is not None, logits.device)
         a = mca_token_logprobs_args(
-            logits.data_ptr(), _dtype_code(logits.dtype), vocab, rows, _ld(logits), t,
-            _addr(r.logprob), r.entropy.data_ptr(), r.lse.data_ptr(), top, _addr(r.top_logprob),
-            _addr(r.top_index), s)
-        _check(load_library().mca_token_logprobs(ctypes.byref(a)))
+            logits.data_ptr(), _dtypes[logits.dtype], vocab, rows, ld, t, _addr(r.logprob),
+            r.entropy.data_ptr(), r.lse.data_ptr(), top, _addr(r.top_logprob), _addr(r.top_index),
+            s)
+        _check(_fn["mca_token_logprobs"](ctypes.byref(a)))
         return r
 
     return _on(dev, stream, call)
@@ -628,25 +645,26 @@ def mca_token_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entr
     """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits, from the
     lse and entropy of mca_token_logprobs. g_logprob (with targets) or g_entropy (with entropy) may be
     None. out: [rows, vocab] of the logits' dtype, which may be `logits` itself."""
-    import torch
-    _cuda("logits", logits, _float_types(), ndim=2)
-    rows, vocab = logits.shape
-    dev = logits.device
+    _ready()
+    rows, vocab, ld = _matrix("logits", logits, _dtypes)
+    dev = logits.get_device()
     f32 = torch.float32
-    v = [_vector("targets", targets, rows, torch.int32, dev),
-         _vector("lse", lse, rows, f32, dev), _vector("entropy", entropy, rows, f32, dev),
-         _vector("g_logprob", g_logprob, rows, f32, dev),
-         _vector("g_entropy", g_entropy, rows, f32, dev)]
+    a = mca_token_logprobs_backward_args(
+        logits.data_ptr(), _dtypes[logits.dtype], vocab, rows, ld,
+        _vector("targets", targets, rows, torch.int32, dev), _vector("lse", lse, rows, f32, dev),
+        _vector("entropy", entropy, rows, f32, dev),
+        _vector("g_logprob", g_logprob, rows, f32, dev),
+        _vector("g_entropy", g_entropy, rows, f32, dev), None, vocab)
     if out is not None:
-        _cuda("out", out, (logits.dtype,), dev, 2)
-        if out.shape != logits.shape:
+        orows, ocols, a.ldg = _matrix("out", out, (logits.dtype,), dev)
+        if orows != rows or ocols != vocab:
             raise ValueError(f"out: shape {tuple(out.shape)}, expected {tuple(logits.shape)}")
 
     def call(s):
-        g = out if out is not None else torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
-        a = mca_token_logprobs_backward_args(logits.data_ptr(), _dtype_code(logits.dtype), vocab,
-                                             rows, _ld(logits), *v, g.data_ptr(), _ld(g), s)
-        _check(load_library().mca_token_logprobs_backward(ctypes.byref(a)))
+        g = out if out is not None else torch.empty((rows, vocab), dtype=logits.dtype,
+                                                    device=logits.device)
+        a.grad, a.stream = g.data_ptr(), s
+        _check(_fn["mca_token_logprobs_backward"](ctypes.byref(a)))
         return g
 
     return _on(dev, stream, call)
@@ -656,7 +674,6 @@ def mca_token_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entr
 def _handle_stream(h: Handle, *inputs):
     """The handle's stream as the current one: its work follows what is queued on the caller's stream
     (which made the inputs), and the caller's stream goes on after it."""
-    import torch
     cur = torch.cuda.current_stream()
     if cur.cuda_stream == h.stream:
         yield []
@@ -676,7 +693,7 @@ def _handle_stream(h: Handle, *inputs):
 def mca_score(h: Handle, top: int = 0):
     """(logits [rows, classes], TokenLogprobs of the labels / next tokens) of the handle's own samples
     under its present weights."""
-    import torch
+    _ready()
     if not 0 <= top <= MAX_TOP:
         raise ValueError(f"top = {top} outside 0..{MAX_TOP}")
     with _handle_stream(h) as made:
@@ -698,16 +715,15 @@ def mca_predict_workspace_size(h: Handle, n: int) -> int:
 def mca_predict(h: Handle, x):
     """Activations [n, n_out] float32 of an MLP handle's last layer for new samples x [n, n_in]
     (float32), every layer in 8-bit integers."""
-    import torch
-    _cuda("x", x, (torch.float32,), ndim=2)
-    if h.n_in and x.shape[1] != h.n_in:
-        raise ValueError(f"x: {x.shape[1]} columns, the net has {h.n_in} inputs")
-    n = x.shape[0]
+    _ready()
+    n, cols, ldx = _matrix("x", x, (torch.float32,))
+    if h.n_in and cols != h.n_in:
+        raise ValueError(f"x: {cols} columns, the net has {h.n_in} inputs")
     with _handle_stream(h, x) as made:
         nbytes = mca_predict_workspace_size(h, n)
         out = torch.empty((n, h.classes), dtype=torch.float32, device="cuda")
         ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-        _check(load_library().mca_predict(h.ptr, x.data_ptr(), n, _ld(x), out.data_ptr(),
+        _check(load_library().mca_predict(h.ptr, x.data_ptr(), n, ldx, out.data_ptr(),
                                           ws.data_ptr() if nbytes else None, nbytes), h.ptr)
         made.append(out)
     return out
