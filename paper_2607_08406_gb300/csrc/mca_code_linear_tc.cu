@@ -1,4 +1,4 @@
-// A layer on 8-bit codes for some dozens of samples, on the tensor cores: 128 outputs by up to 64 samples per CTA, the
+// A layer on 8-bit codes for some dozens of samples, on the tensor cores: 128 outputs by up to 128 samples per CTA, the
 // columns split over the CTAs of a cluster where tiles are few.
 //
 // The transposed tile D[128 outputs x T samples] = W X^T is what a CTA computes, so that the weights, which are
@@ -26,10 +26,10 @@ namespace {
 constexpr int kStageK = 128;                  // columns per stage
 constexpr int kRowsWarp = 16;                 // rows that a warp converts
 constexpr int kWWarps = kM / kRowsWarp;
-constexpr int kNC = 2;                        // stages
 
 template <int T>
 struct Shape {
+  static constexpr int kNC = T > 64 ? 3 : 2;                   // stages
   static constexpr int kXWarps = T / kRowsWarp;
   static constexpr int kConvWarps = kWWarps + kXWarps;
   static constexpr int kThreads = 32 * (kConvWarps + 1);       // and one warp that issues MMAs
@@ -38,6 +38,8 @@ struct Shape {
   static constexpr uint32_t kStage = kW + (kStageK / 8) * kLboX;
   static constexpr uint32_t kSmem = kNC * kStage + 128;
   static constexpr uint32_t kTmem = 2 * T;      // the sums of the MMAs, and whole sums as integers
+  static constexpr int kParts = T > 64 ? 4 : 2;                // of the samples, of which a warp takes one's sums
+  static constexpr int kGroups = kConvWarps / 4;               // of 128 threads that write outputs
   static_assert(kNC * kStage >= T * kM * 4, "the parts of a split sum take the place of the stages");
 };
 
@@ -71,12 +73,14 @@ struct Codes {
 };
 
 template <int T, int DT>
-__global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kernel(SplitArgs p) {
+__global__ void __launch_bounds__(Shape<T>::kThreads, T > 64 ? 1 : 2) code_linear_split_kernel(SplitArgs p) {
   using S = Shape<T>;
+  constexpr int kNC = S::kNC;
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[kNC], s_free[kNC], s_sum, s_taken;
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
+  __shared__ float s_scale[T];
   const mca_code_linear_args& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = p.splits > 1 ? (int)cluster_rank() : 0;
@@ -101,17 +105,17 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kerne
       mbar_init(&s_free[q], 1);
     }
     mbar_init(&s_sum, 1);
-    mbar_init(&s_taken, kWWarps);
+    mbar_init(&s_taken, 4 * S::kParts);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_fail = 0;
   }
+  if (tid < nt) s_scale[tid] = __ldg(a.x_scale + r0 + tid);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
 
-  constexpr int kHalf = T / 2;
-  const int half = warp >> 2;                              // of the samples, in the weights' warps
+  constexpr int kPart = T / S::kParts;
 
   if (warp == S::kConvWarps) {
     if (elect_one()) {
@@ -135,7 +139,7 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kerne
         if (in == kPer - 1 || c == nst - 1) umma_commit(&s_sum);
       }
     }
-  } else if (warp < kWWarps + n16 / kRowsWarp) {
+  } else {
     const bool isx = warp >= kWWarps;
     const int t = lane & 3, row = (isx ? warp - kWWarps : warp) * kRowsWarp + (lane >> 2);
     // rows behind the last are read as the last; their sums are not used
@@ -144,13 +148,15 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kerne
     const int8_t* const p1 = isx ? a.x + (r0 + min(row + 8, nt - 1)) * a.ldx
                                  : a.w + (int64_t)min(n0 + row + 8, a.n_out - 1) * a.ldw;
     const uint32_t lbo = isx ? S::kLboX : S::kLboW;
+    const bool has = !isx || row < n16, sums = warp < 4 * S::kParts;
     bool ok = true;
     // two stages of codes on their way: each is asked for when the one before the last has been stored
     Codes even, odd;
     auto load = [&](Codes& v, int c) {
-      if (c < nst) v.load(p0, p1, (c0 + c) * kStageK + 16 * t, a.n_in);
+      if (has && c < nst) v.load(p0, p1, (c0 + c) * kStageK + 16 * t, a.n_in);
     };
     auto convert = [&](Codes& v, int c) {
+      if (!has) return;
       const int st = c % kNC;
       if (c >= kNC) ok = warp_all(mbar_wait(&s_free[st], (uint32_t)(c / kNC - 1) & 1u));
       if (!ok) return;
@@ -165,29 +171,34 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kerne
       convert(even, c);
       if (ok && c + 1 < nst) convert(odd, c + 1);
       const int last = min(c + 1, nst - 1);
-      if (!isx && ok && (last % kPer == kPer - 1 || last == nst - 1)) {   // an exact sum is complete
+      if (sums && ok && (last % kPer == kPer - 1 || last == nst - 1)) {   // an exact sum is complete
         ok = warp_all(mbar_wait(&s_sum, (uint32_t)(last / kPer) & 1u));
         if (!ok) break;
         tc_fence_after();
         // added to what is there already; the last one leaves for shared memory, [sample][output], in the place
         // of the stages, which the MMAs have read
-        const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kHalf);
-        const int out = (warp & 3) * 32 + lane;
+        const int t0 = (warp >> 2) * kPart;
+        const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)t0;
+        const uint32_t to = buf + (uint32_t)(t0 * kM + (warp & 3) * 32 + lane) * 4u;
 #pragma unroll 1
-        for (int q = 0; q < kHalf && half * kHalf + q < n16; q += 16) {
+        for (int q = 0; q < kPart && t0 + q < n16; q += 16) {
           float d[16], e[16];
           tmem_ld16(from + (uint32_t)q, d);
           if (last >= kPer) tmem_ld16(from + (uint32_t)(T + q), e);
+          int v[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int s = __float2int_rn(d[i]) + (last >= kPer ? __float_as_int(e[i]) : 0);
-            e[i] = __int_as_float(s);
-            if (last == nst - 1 && half * kHalf + q + i < nt)
-              asm volatile("st.shared.s32 [%0], %1;"
-                           ::"r"(buf + (uint32_t)((half * kHalf + q + i) * kM + out) * 4u), "r"(s)
+          for (int i = 0; i < 16; ++i)
+            v[i] = __float2int_rn(d[i]) + (last >= kPer ? __float_as_int(e[i]) : 0);
+          if (last == nst - 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              asm volatile("st.shared.s32 [%0], %1;" ::"r"(to + (uint32_t)((q + i) * kM) * 4u), "r"(v[i])
                            : "memory");
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) e[i] = __int_as_float(v[i]);
+            tmem_st16(from + (uint32_t)(T + q), e);
           }
-          if (last < nst - 1) tmem_st16(from + (uint32_t)(T + q), e);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
@@ -195,39 +206,46 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, 2) code_linear_split_kerne
       }
     }
     // every MMA's arrival comes before the CTA leaves
-    for (int c = max(0, nst - kNC); c < nst && ok; ++c)
+    for (int c = max(0, nst - kNC); c < nst && ok && has; ++c)
       ok = warp_all(mbar_wait(&s_free[c % kNC], (uint32_t)(c / kNC) & 1u));
     if (!ok) s_fail = 1;
   }
   __syncwarp();
   __syncthreads();
-  const bool fail = s_fail != 0;
-  const int ch = tid & 127, n = n0 + ch;
-  if (p.splits > 1)
+  bool fail = s_fail != 0;
+  if (p.splits > 1) {
     cluster_sync_all();
-  else
-    __syncthreads();
-  if (tid < 256 && n < a.n_out) {
+    for (int q = 0; q < p.splits; ++q) fail |= ld_cluster(smem_u32(&s_fail), q) != 0;
+  }
+  const int ch = tid & 127, grp = tid >> 7, n = n0 + ch;
+  if (grp < S::kGroups && n < a.n_out) {
     const float ws = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.0f;
-    elem_t<DT>* y = static_cast<elem_t<DT>*>(a.y) + r0 * a.ldy + n;
-    // any CTA of a cluster that failed: its part is missing in every sample
-    const int step = fail ? 2 : 2 * p.splits;
-    for (int t0 = fail ? half : rank * 2 + half; t0 < nt; t0 += 4 * step) {
-      float z[4];
+    const int step = S::kGroups * p.splits;
+    int t = rank * S::kGroups + grp;
+    elem_t<DT>* y = static_cast<elem_t<DT>*>(a.y) + (r0 + t) * a.ldy + n;
+    const int64_t ystep = (int64_t)step * a.ldy;
+    uint32_t at = buf + (uint32_t)(t * kM + ch) * 4u;
+    for (; t < nt; t += 8 * step, at += (uint32_t)(8 * step * kM) * 4u) {
+      int v[8];
+      float z[8];
+      if (p.splits == 1) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = min(t0 + i * step, nt - 1);
-        int s = 0;
-        if (p.splits > 1)
-          for (int q = 0; q < p.splits; ++q) s += ld_cluster(buf + (uint32_t)(t * kM + ch) * 4u, q);
-        else
-          s = ld_shared(buf + (uint32_t)(t * kM + ch) * 4u);
-        z[i] = code_field(__int2float_rn(s), __ldg(a.x_scale + r0 + t), ws, b, a.bias != nullptr);
+        for (int i = 0; i < 8; ++i) v[i] = t + i * step < nt ? ld_shared(at + (uint32_t)(i * step * kM) * 4u) : 0;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0;
+        for (int q = 0; q < p.splits; ++q)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (t + i * step < nt) v[i] += ld_cluster(at + (uint32_t)(i * step * kM) * 4u, q);
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        z[i] = code_field(__int2float_rn(v[i]), s_scale[min(t + i * step, T - 1)], ws, b, a.bias != nullptr);
       act_block(z, a.act, a.act_param);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (t0 + i * step < nt) y[(t0 + i * step) * a.ldy] = elem_of<DT>(fail ? NAN : z[i]);
+      for (int i = 0; i < 8; ++i, y += ystep)
+        if (t + i * step < nt) *y = elem_of<DT>(fail ? NAN : z[i]);
     }
   }
   tc_fence_before();
@@ -274,15 +292,15 @@ cudaError_t launch_split_t(const SplitArgs& p, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s) {
-  const int T = a.rows <= 32 ? 32 : 64;
+  const int T = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128, per_sm = T > 64 ? 1 : 2;
   SplitArgs p{};
   p.a = a;
   p.stages = (a.n_in + kStageK - 1) / kStageK;
-  // clusters of up to 8 CTAs while two CTAs per SM have no tile of their own, two stages each at least
+  // clusters of up to 8 CTAs while places for CTAs have no tile of their own, two stages each at least
   const int64_t tiles = (int64_t)((a.n_out + kM - 1) / kM) * ((a.rows + T - 1) / T);
   p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= 2 * 152 && p.stages >= 4 * p.splits) p.splits *= 2;
-  return T == 32 ? launch_split_t<32>(p, s) : launch_split_t<64>(p, s);
+  while (p.splits < 8 && tiles * p.splits * 2 <= per_sm * 152 && p.stages >= 4 * p.splits) p.splits *= 2;
+  return T == 32 ? launch_split_t<32>(p, s) : T == 64 ? launch_split_t<64>(p, s) : launch_split_t<128>(p, s);
 }
 
 }  // namespace mca
