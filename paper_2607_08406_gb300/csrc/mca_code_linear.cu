@@ -8,10 +8,30 @@ namespace {
 
 enum class Kernel { kStream, kSplit, kPair };
 
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The kernel by sizes, from times measured on GB300 (us; stream / cluster / pair):
+//   rows   n_in n_out              rows    n_in n_out
+//     16   4096  4096   9.5 / 12     16   16384  1024  27 / 17
+//     64   1024  1024   6.7 / 9      64    8192  8192  52 / 33
+//    256   1024  1024   7.0 / 10 / 13    64   4096 16384  57 / 34 / 61
+//    128   8192  8192  102 / 39 / 74    512    8192  8192  - / 146 / 77
+//    256   4096  4096   57 / 23 / 33    512    4096  4096  - / 38 / 34
+//    512  16384  1024  100 / 40 / 86    128     784  4096  14 / 13 / 12
+// Few samples stream the weights, as long as a CTA's 32 outputs by 64 samples all run at once and their columns
+// are not too many; beyond, the cluster kernel takes about 7 us and 1.03 us for each of its stages of 128 columns,
+// the pair kernel 9 us, the operands' way to fp16 and back (3 bytes a code) and 4.1 ns for each column of its
+// rounds of tiles.
 Kernel choose(const mca_code_linear_args& a) {
-  const double w = (double)a.n_in * a.n_out;
-  if (a.rows <= 32 || (a.rows <= 64 && w <= 16e6) || (a.rows <= 256 && w <= 1.1e6)) return Kernel::kStream;
-  return a.rows > 96 ? Kernel::kPair : Kernel::kSplit;
+  const int64_t rows = a.rows, n_in = a.n_in, n_out = a.n_out, sms = 152;
+  if (rows <= 8) return Kernel::kStream;
+  if (rows <= 32) return n_in <= 8192 ? Kernel::kStream : Kernel::kSplit;
+  if (n_in <= 2560 && ceil_div(n_out, 32) * ceil_div(rows, 64) <= sms) return Kernel::kStream;
+  if (rows <= 64) return Kernel::kSplit;
+  const double split = 7.0 + 1.03 * code_linear_split_stages(a);
+  const double pair = 9.0 + 3.0 * (double)n_in * (double)(n_out + rows) / 5.5e6 +
+                      0.0041 * (double)(ceil_div(ceil_div(n_out, 256) * ceil_div(rows, 256), sms / 2) * n_in);
+  return split < pair ? Kernel::kSplit : Kernel::kPair;
 }
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }

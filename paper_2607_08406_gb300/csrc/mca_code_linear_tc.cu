@@ -289,18 +289,40 @@ cudaError_t launch_split_t(const SplitArgs& p, cudaStream_t s) {
   }
 }
 
+constexpr int kSms = 152;
+
+// Samples per tile, and CTAs per cluster: up to 8 while places for CTAs have no tile of their own, two stages
+// each at least.
+struct Plan {
+  int T, per_sm, splits, stages;
+  int64_t tiles;
+  explicit Plan(const mca_code_linear_args& a) {
+    T = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+    per_sm = T > 64 ? 1 : 2;
+    stages = (a.n_in + kStageK - 1) / kStageK;
+    tiles = (int64_t)((a.n_out + kM - 1) / kM) * ((a.rows + T - 1) / T);
+    splits = 1;
+    while (splits < 8 && tiles * splits * 2 <= per_sm * kSms && stages >= 4 * splits) splits *= 2;
+  }
+};
+
 }  // namespace
 
+double code_linear_split_stages(const mca_code_linear_args& a) {
+  const Plan p(a);
+  const int64_t places = p.per_sm * kSms;
+  return (double)((p.tiles * p.splits + places - 1) / places) * (double)((p.stages + p.splits - 1) / p.splits);
+}
+
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s) {
-  const int T = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128, per_sm = T > 64 ? 1 : 2;
+  const Plan plan(a);
   SplitArgs p{};
   p.a = a;
-  p.stages = (a.n_in + kStageK - 1) / kStageK;
-  // clusters of up to 8 CTAs while places for CTAs have no tile of their own, two stages each at least
-  const int64_t tiles = (int64_t)((a.n_out + kM - 1) / kM) * ((a.rows + T - 1) / T);
-  p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= per_sm * 152 && p.stages >= 4 * p.splits) p.splits *= 2;
-  return T == 32 ? launch_split_t<32>(p, s) : T == 64 ? launch_split_t<64>(p, s) : launch_split_t<128>(p, s);
+  p.stages = plan.stages;
+  p.splits = plan.splits;
+  return plan.T == 32   ? launch_split_t<32>(p, s)
+         : plan.T == 64 ? launch_split_t<64>(p, s)
+                        : launch_split_t<128>(p, s);
 }
 
 }  // namespace mca
