@@ -416,7 +416,7 @@ mca_status mca_quantize_rows(const void* x, int32_t dtype, int64_t rows, int64_t
  * and y to `dtype` (to an infinity beyond fp16's range). */
 typedef struct {
   int64_t rows;            /* samples or tokens */
-  int32_t n_in, n_out;     /* 1 <= n_in <= 131071: sums of any codes stay below 2^31 */
+  int32_t n_in, n_out;     /* 1 <= n_in <= 131071 (sums of any codes stay below 2^31), 1 <= n_out <= 2^30 */
   const int8_t* x;         /* [rows x n_in] */
   int64_t ldx;
   const float* x_scale;    /* [rows] */

@@ -117,7 +117,8 @@ mca_status check_linear(const mca_code_linear_args* a) {
   MCA_CHECK(check_rows(nullptr, a->rows));
   if (a->n_in < 1 || a->n_in > 131071)
     return fail(nullptr, MCA_ERR_INVALID, "n_in = %d outside 1..131071", a->n_in);
-  if (a->n_out < 1) return fail(nullptr, MCA_ERR_INVALID, "n_out = %d", a->n_out);
+  if (a->n_out < 1 || a->n_out > 1 << 30)
+    return fail(nullptr, MCA_ERR_INVALID, "n_out = %d outside 1..2^30", a->n_out);
   MCA_CHECK(check_dtype(a->dtype));
   if (a->act < MCA_ACT_IDENTITY || a->act > MCA_ACT_GELU)
     return fail(nullptr, MCA_ERR_INVALID, "unknown transfer function %d", a->act);
@@ -250,12 +251,15 @@ PredictPlan predict_plan(const mca_handle* h, int64_t n) {
   p.w_scale = take(4 * outs);
   size_t product = 0;
   for (const mca_layer& L : h->layers) {
-    mca_code_linear_args a{};
-    a.rows = p.chunk;
-    a.n_in = L.n_in;
-    a.n_out = L.n_out;
-    a.ldx = a.ldw = round16(L.n_in);
-    product = std::max(product, mca::code_linear_workspace(a));
+    for (const int64_t rows : {p.chunk, n % p.chunk}) {        // every pass, and the last one
+      if (rows == 0) continue;
+      mca_code_linear_args a{};
+      a.rows = rows;
+      a.n_in = L.n_in;
+      a.n_out = L.n_out;
+      a.ldx = a.ldw = round16(L.n_in);
+      product = std::max(product, mca::code_linear_workspace(a));
+    }
   }
   p.product = take(product);
   p.total = at;

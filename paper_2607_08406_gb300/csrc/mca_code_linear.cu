@@ -19,8 +19,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 //    256   4096  4096   57 / 23 / 33    512    4096  4096  - / 38 / 34
 //    512  16384  1024  100 / 40 / 86    128     784  4096  14 / 13 / 12
 // Few samples stream the weights, as long as a CTA's 32 outputs by 64 samples all run at once and their columns
-// are not too many; beyond, the cluster kernel takes about 7 us and 1.03 us for each of its stages of 128 columns,
-// the pair kernel 9 us, the operands' way to fp16 and back (3 bytes a code) and 4.1 ns for each column of its
+// are not too many; beyond, the cluster kernel takes about 3 us and, for each round of its CTAs, 4 us and 1.03 us for
+// every stage of 128 columns, the pair kernel 9 us, the operands' way to fp16 and back (3 bytes a code) and 4.1 ns for each column of its
 // rounds of tiles.
 Kernel choose(const mca_code_linear_args& a) {
   const int64_t rows = a.rows, n_in = a.n_in, n_out = a.n_out, sms = 152;
@@ -28,7 +28,7 @@ Kernel choose(const mca_code_linear_args& a) {
   if (rows <= 32) return n_in <= 8192 ? Kernel::kStream : Kernel::kSplit;
   if (n_in <= 2560 && ceil_div(n_out, 32) * ceil_div(rows, 64) <= sms) return Kernel::kStream;
   if (rows <= 64) return Kernel::kSplit;
-  const double split = 7.0 + 1.03 * code_linear_split_stages(a);
+  const double split = code_linear_split_us(a);
   const double pair = 9.0 + 3.0 * (double)n_in * (double)(n_out + rows) / 5.5e6 +
                       0.0041 * (double)(ceil_div(ceil_div(n_out, 256) * ceil_div(rows, 256), sms / 2) * n_in);
   return split < pair ? Kernel::kSplit : Kernel::kPair;

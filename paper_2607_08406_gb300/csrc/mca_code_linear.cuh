@@ -127,9 +127,8 @@ inline bool code_rows_aligned(const int8_t* p, int64_t rows, int64_t ld) {
 
 // mca_code_linear_stream.cu: few samples; operands' rows on 16-byte boundaries.
 cudaError_t launch_code_linear_stream(const mca_code_linear_args& a, cudaStream_t s);
-// mca_code_linear_tc.cu: some dozens of samples; operands' rows on 16-byte boundaries. Stages: of 128 columns that
-// an SM goes through one after the other.
-double code_linear_split_stages(const mca_code_linear_args& a);
+// mca_code_linear_tc.cu: some dozens of samples; operands' rows on 16-byte boundaries. Its time by sizes.
+double code_linear_split_us(const mca_code_linear_args& a);
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s);
 // mca_code_linear_pair.cu: many samples; in a.workspace the operands as fp16.
 size_t code_linear_pair_workspace(const mca_code_linear_args& a);

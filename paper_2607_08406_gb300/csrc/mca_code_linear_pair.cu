@@ -11,8 +11,8 @@
 // Bulk copies bring chunks (16 KB of each operand) into a ring of six stages. The sums have two places in tensor
 // memory (2 x 256 columns): while one is read, scaled and written, the next tile's MMAs run.
 //
-// Warps: 0 copies, 1 issues MMAs (the pair's first CTA), 4-11 take the sums (each 32 outputs and half of the
-// samples). Sums of more than 1024 columns are added up as integers in registers and returned to tensor memory as fp32,
+// Warps: 0 copies, 1 issues MMAs (the pair's first CTA), 4-19 take the sums (each 32 outputs and a
+// quarter of the samples). Sums of more than 1024 columns are added up as integers in registers and returned to tensor memory as fp32,
 // from where the outputs are written in one loop.
 //
 // Every wait is bounded (2 s). After one that ran out the later ones do too, and the outputs not yet written
@@ -27,8 +27,9 @@ namespace {
 
 constexpr int kTB = 128;                        // samples per CTA
 constexpr int kT = 2 * kTB;                     // samples per tile (MMA N)
-constexpr int kPairThreads = 384;
-constexpr int kFirstSum = 4;                    // first warp of those that take the sums
+constexpr int kFirstSum = 4, kSumWarps = 16;    // warps that take the sums
+constexpr int kPart = kT / (kSumWarps / 4);     // samples of one
+constexpr int kPairThreads = 32 * (kFirstSum + kSumWarps);
 constexpr int kSubK = 64;                       // columns per chunk
 constexpr int kStages = 6;
 constexpr uint32_t kChunk = kM * kSubK * 2;     // bytes of a block's chunk of 64 columns
@@ -152,7 +153,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_free[kStages], s_sum[2], s_taken[2];
   __shared__ uint32_t s_tmem;
-  __shared__ float s_scale[8][kTB];             // of a tile's samples, for each warp that takes sums
+  __shared__ float s_scale[kSumWarps][kPart];   // of a tile's samples, for each warp that takes sums
   const mca_code_linear_args& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_rank();
@@ -174,7 +175,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
     for (int q = 0; q < 2; ++q) {
       mbar_init(&s_sum[q], 1);
-      mbar_init(&s_taken[q], 16);                 // the warps of both CTAs
+      mbar_init(&s_taken[q], 2 * kSumWarps);      // of both CTAs
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -246,7 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kFirstSum) {
-    const int half = (warp - kFirstSum) >> 2;
+    const int part = (warp - kFirstSum) >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
     int d = 0;
@@ -255,31 +256,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int64_t r0;
       tile_at(p, i, &n0, &r0);
       const int n = n0 + rank * kM + (warp & 3) * 32 + lane;
-      r0 += half * kTB;
-      const int nt = (int)max((int64_t)0, min((int64_t)kTB, a.rows - r0));
+      r0 += part * kPart;
+      const int nt = (int)max((int64_t)0, min((int64_t)kPart, a.rows - r0));
       float* const xs = s_scale[warp - kFirstSum];
       __syncwarp();
 #pragma unroll
-      for (int q = 0; q < kTB; q += 32)
+      for (int q = 0; q < kPart; q += 32)
         if (q + lane < nt) xs[q + lane] = __ldg(a.x_scale + r0 + q + lane);
       __syncwarp();
       uint32_t from = 0u;
       if (nsum == 1) {
         ok = ok && warp_all(wait_pair(&s_sum[d & 1], (uint32_t)(d >> 1) & 1u));
         tc_fence_after();
-        from = tmem + lanes + (uint32_t)(d & 1) * kT + (uint32_t)(half * kTB);
+        from = tmem + lanes + (uint32_t)(d & 1) * kT + (uint32_t)(part * kPart);
         ++d;
       } else {
-        int acc[kTB];
+        int acc[kPart];
 #pragma unroll
-        for (int q = 0; q < kTB; ++q) acc[q] = 0;
+        for (int q = 0; q < kPart; ++q) acc[q] = 0;
         for (int m = 0; m < nsum; ++m, ++d) {
           ok = ok && warp_all(wait_pair(&s_sum[d & 1], (uint32_t)(d >> 1) & 1u));
           if (!ok) break;
           tc_fence_after();
-          from = tmem + lanes + (uint32_t)(d & 1) * kT + (uint32_t)(half * kTB);
+          from = tmem + lanes + (uint32_t)(d & 1) * kT + (uint32_t)(part * kPart);
 #pragma unroll
-          for (int q = 0; q < kTB; q += 16) {
+          for (int q = 0; q < kPart; q += 16) {
             float v[16];
             tmem_ld16(from + (uint32_t)q, v);
 #pragma unroll
@@ -292,7 +293,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         }
         if (ok) {
 #pragma unroll
-          for (int q = 0; q < kTB; q += 16) {
+          for (int q = 0; q < kPart; q += 16) {
             float v[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) v[k] = __int2float_rn(acc[q + k]);

@@ -308,10 +308,10 @@ struct Plan {
 
 }  // namespace
 
-double code_linear_split_stages(const mca_code_linear_args& a) {
+double code_linear_split_us(const mca_code_linear_args& a) {
   const Plan p(a);
-  const int64_t places = p.per_sm * kSms;
-  return (double)((p.tiles * p.splits + places - 1) / places) * (double)((p.stages + p.splits - 1) / p.splits);
+  const int64_t places = p.per_sm * kSms, rounds = (p.tiles * p.splits + places - 1) / places;
+  return 3.0 + (double)rounds * (4.0 + 1.03 * (double)((p.stages + p.splits - 1) / p.splits));
 }
 
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s) {

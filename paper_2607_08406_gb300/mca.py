@@ -422,8 +422,8 @@ def mca_selftest_wait_timeout():
 
 # ------------------------------------------------------------------------------------------------
 # A trained net's answers. Tensors are CUDA tensors of one device, matrices with unit column stride;
-# results are new tensors (or the ones given). Work is queued on `stream` (a cudaStream_t, default:
-# the device's current torch stream), and tensors made here belong to it.
+# results are new tensors (or the ones given). Work is queued on `stream` (a torch.cuda.Stream or
+# cudaStream_t, default: the device's current torch stream), and tensors made here belong to it.
 # ------------------------------------------------------------------------------------------------
 
 torch = None             # the module, once one of the calls below has needed it
@@ -488,6 +488,8 @@ def _dtype_code(dtype) -> int:
 
 def _on(index, stream, call):
     """call(stream's cudaStream_t) with device `index` current and tensors allocated on the stream."""
+    if stream is not None:
+        stream = getattr(stream, "cuda_stream", stream)
     if torch._C._cuda_getDevice() == index:
         cur = torch._C._cuda_getCurrentRawStream(index)
         if stream is None or stream == cur:

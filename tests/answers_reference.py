@@ -26,7 +26,11 @@ def quantize(x):
 
 
 def _erfc(z):
-    return np.vectorize(math.erfc)(z)
+    try:
+        import torch
+        return torch.erfc(torch.from_numpy(np.ascontiguousarray(z))).numpy()
+    except ImportError:
+        return np.vectorize(math.erfc)(z)
 
 
 def act(name, z, g):
@@ -46,7 +50,11 @@ def act(name, z, g):
 
 def code_linear(xq, xs, wq, ws, bias, name, g, dtype):
     """(y, how far an output may be off)."""
-    s = xq.astype(np.int64) @ wq.astype(np.int64).T
+    return code_fields(xq.astype(np.int64) @ wq.astype(np.int64).T, xs, ws, bias, name, g, dtype)
+
+
+def code_fields(s, xs, ws, bias, name, g, dtype):
+    """The same from the integer sums."""
     z0 = s.astype(np.float64) * xs.astype(np.float64)[:, None] * ws.astype(np.float64)
     z = z0 if bias is None else z0 + bias.astype(np.float64)
     # the sum to fp32, two products, one addition

@@ -78,6 +78,7 @@ def test_code_linear_refusals(lib):
         mca.MCA_ERR_INVALID
     for kw, word in [(dict(rows=-1), b"rows"), (dict(n_in=0), b"n_in"),
                      (dict(n_in=131072, ldx=131072, ldw=131072), b"n_in"), (dict(n_out=0), b"n_out"),
+                     (dict(n_out=(1 << 30) + 1, ldy=1 << 31), b"n_out"),
                      (dict(dtype=5), b"dtype"), (dict(act=6), b"transfer"),
                      (dict(act=-1), b"transfer"), (dict(ldx=15), b"x: row"),
                      (dict(ldw=15), b"w: row"), (dict(ldy=2), b"y: row")]:
@@ -115,6 +116,7 @@ def test_token_logprobs_refusals(lib):
     assert lib.mca_token_logprobs(None) == mca.MCA_ERR_INVALID
     assert lib.mca_token_logprobs(ctypes.byref(logprob_args(rows=0, logits=None))) == mca.MCA_OK
     for kw, word in [(dict(dtype=9), b"dtype"), (dict(rows=-2), b"rows"), (dict(vocab=0), b"vocab"),
+                     (dict(vocab=(1 << 30) + 1, ld=1 << 31), b"vocab"),
                      (dict(ld=7), b"logits: row"), (dict(top=-1), b"top"), (dict(top=33), b"top"),
                      (dict(top=0), b"top = 0"), (dict(targets=None), b"targets"),
                      (dict(logits=None), b"logits is NULL"),

@@ -206,6 +206,57 @@ def test_code_linear_largest_sums(gpu_lib, rows, n_in, code):
     assert np.array_equal(got, s.astype(np.float32).astype(np.float64))
 
 
+def sums_on_gpu(xq, wq):
+    """Integer sums in fp64, which holds them exactly."""
+    return (xq.double() @ wq.double().T)
+
+
+@pytest.mark.parametrize("dtype,act,g,bias", [("float32", "identity", 0.0, False),
+                                              ("float16", "gaussian", 1.0, False),
+                                              ("bfloat16", "gelu", 0.0, True),
+                                              ("float32", "tanh", 0.0, True)])
+@pytest.mark.parametrize("rows,n_in,n_out,off,pad", [
+    # tiles of the pair kernel: whole, ragged, of one to six exact sums, rows off 16-byte boundaries
+    (2048, 1024, 2048, (0, 0, 0), 0), (2491, 432, 5121, (0, 0, 0), 3), (5901, 176, 2687, (1, 0, 1), 0),
+    (700, 2992, 4000, (0, 7, 0), 0), (1501, 5001, 3003, (0, 0, 3), 1), (3086, 64, 10970, (0, 0, 0), 0),
+    # of the cluster kernel, up to 128 samples and more
+    (57, 4880, 6140, (0, 0, 0), 0), (36, 11808, 1660, (5, 0, 0), 0), (105, 4992, 3096, (0, 0, 1), 2),
+    (128, 3001, 500, (0, 3, 0), 0), (300, 8192, 700, (0, 0, 0), 0), (65, 131071, 129, (0, 0, 0), 0)])
+def test_code_linear_many(gpu_lib, rows, n_in, n_out, off, pad, dtype, act, g, bias):
+    """Sizes beyond the numpy form: its formula on sums that the GPU makes in fp64, from codes of one sign
+    and of both."""
+    import torch
+    rng = np.random.default_rng(rows + n_in)
+    xq, wq, xs, ws = linear_case(rng, rows, n_in, n_out)
+    xq[: rows // 2] = np.abs(xq[: rows // 2])
+    wq[: n_out // 2] = np.abs(wq[: n_out // 2])
+    b = rng.standard_normal(n_out).astype(np.float32) if bias else None
+    got = run_linear(gpu_lib, xq, wq, xs, ws, b, act, g, dtype, off=off, pad=pad)
+    s = sums_on_gpu(torch.from_numpy(xq).cuda(), torch.from_numpy(wq).cuda()).cpu().numpy()
+    if act == "identity" and b is None:
+        want = (s.astype(np.float32) * xs[:, None]) * ws
+        assert np.array_equal(got, want.astype(np.float64))
+        return
+    want, tol = R.code_fields(s, xs, ws, b, act, g, dtype)
+    assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(2048, 1040, 2048), (1500, 5000, 3000), (100, 9000, 600)])
+@pytest.mark.parametrize("code", [-128, 127])
+def test_code_linear_largest_sums_of_many(gpu_lib, rows, n_in, n_out, code):
+    import torch
+    rng = np.random.default_rng(n_in)
+    xq = np.full((rows, n_in), code, np.int8)
+    wq = np.full((n_out, n_in), code, np.int8)
+    wq[:, 0] = rng.integers(-128, 128, n_out)
+    xq[:, 1] = rng.integers(-128, 128, rows)
+    xq[:, 0] = 1
+    got = run_linear(gpu_lib, xq, wq, np.ones(rows, np.float32), np.ones(n_out, np.float32), None,
+                     "identity", 0.0, "float32")
+    s = sums_on_gpu(torch.from_numpy(xq).cuda(), torch.from_numpy(wq).cuda()).cpu().numpy()
+    assert np.array_equal(got, s.astype(np.float32).astype(np.float64))
+
+
 def test_code_linear_scales(gpu_lib):
     """Scales of zero, tiny and huge magnitude, infinities and NaN go through by IEEE rules."""
     rng = np.random.default_rng(3)
@@ -474,6 +525,9 @@ def test_stream_and_graph(gpu_lib, rows, n_in, vocab, ldw):
     got = answers(gpu_lib, x, w, ws, t, stream=side.cuda_stream)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = answers(gpu_lib, x, w, ws, t, stream=side)             # the stream itself
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
     buf = x.clone()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -514,7 +568,8 @@ def test_same_results_again(gpu_lib):
     """No order of arrival changes a result: ten calls agree bit for bit."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(0)
-    for rows, n_in, vocab in ((1, 4096, 50001), (17, 2048, 4096), (600, 1500, 700)):
+    for rows, n_in, vocab in ((1, 4096, 50001), (17, 2048, 4096), (600, 1500, 700), (100, 5000, 3001),
+                              (2000, 512, 3001)):
         x = torch.randn(rows, n_in, generator=g, device="cuda")
         w = torch.randint(-127, 128, (vocab, n_in), generator=g, device="cuda").to(torch.int8)
         ws = torch.rand(vocab, generator=g, device="cuda") * 1e-3

@@ -138,11 +138,11 @@ def test_predict_in_passes(gpu_lib):
     wl = net(rng, (24, 4096, 3), "tanh", "identity", "softmax_ce", 64)
     st = torch.cuda.Stream()
     h = gpu_lib.create_from_workload(wl, stream=st.cuda_stream)
-    n = 20001
-    x = torch.randn(n, 24, device="cuda")
-    got = gpu_lib.mca_predict(h, x)
-    ref = layer_by_layer(gpu_lib, wl, gpu_lib.mca_get_params(h, wl.n_params), None, x)
-    assert torch.equal(got, ref)
+    x = torch.randn(20001, 24, device="cuda")
+    for n in (20001, 16384, 8200):
+        got = gpu_lib.mca_predict(h, x[:n])
+        ref = layer_by_layer(gpu_lib, wl, gpu_lib.mca_get_params(h, wl.n_params), None, x[:n])
+        assert torch.equal(got, ref)
     logits, r = gpu_lib.mca_score(h, 2)
     assert logits.shape == (64, 3) and r.top_index.shape == (64, 2)
     assert abs(-float(r.logprob.double().mean()) - gpu_lib.mca_loss(h)) <= 1e-5
