@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kAhead = 6;                 // pieces that a thread has on their way
+constexpr int kAhead = 4;                 // pieces that a thread has on their way
 constexpr int kGroups = 8;                // groups of a thread's pieces
 constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary
 
@@ -538,39 +538,46 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
     // kAhead pieces on their way to shared memory, each to its thread's own places: no registers, no barriers. A piece at an
     // end of the row that is not whole is put there by its thread.
     const unsigned int ring = (unsigned int)__cvta_generic_to_shared(&s_ring[0][tid]);
-    int j = j0 + tid, slot = 0;
-    auto ask = [&](int at) {
-      if (at < j1) {
-        const unsigned int to = ring + (unsigned int)(slot * kTeam * 16);
-        if (row.whole(at)) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row.pieces() + at) : "memory");
+    constexpr unsigned int kSlot = kTeam * 16;
+    const int w0 = row.whole(0) ? 0 : 1, whole = row.count - w0 - (row.whole(row.count - 1) ? 0 : 1);
+    unsigned int slot = ring;
+    int j = j0 + tid, next = j;
+    const uint4* x = row.pieces() + j;                          // of piece `next`
+    auto ask = [&] {
+      if (next < j1) {
+        if ((unsigned int)(next - w0) < (unsigned int)whole) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(x) : "memory");
         } else {
-          const uint4 q = row.part(at);
+          const uint4 q = row.part(next);
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
-                       ::"r"(to), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+                       ::"r"(slot), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
-      slot = slot + 1 == kAhead ? 0 : slot + 1;
+      next += kTeam;
+      x += kTeam;
+      slot = slot == ring + (kAhead - 1) * kSlot ? ring : slot + kSlot;
     };
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) ask(j + i * kTeam);
+    for (int i = 0; i < kAhead; ++i) ask();
     float b = -INFINITY;                                        // the group's largest
-    int left = size, group = 0;
+    int left = size;
+    float* group = &s.top[0][tid];
     for (; j < j1; j += kTeam) {
       uint4 q;
       asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
-                   : "r"(ring + (unsigned int)(slot * kTeam * 16)) : "memory");
+                   : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(slot) : "memory");
       b = fmaxf(b, seen.take(q, j));
-      if (--left == 0 || j + kTeam >= j1) {
-        s.top[group++][tid] = b;
+      if (--left == 0) {
+        *group = b;
+        group += kTeam;
         b = -INFINITY;
         left = size;
       }
-      ask(j + kAhead * kTeam);
+      ask();
     }
+    if (left < size) *group = b;
   }
   __syncwarp();
   Sums t = team_sums<W>(seen.sums(), s);
@@ -699,7 +706,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_small_kernel(mca_t
 }
 
 // kAhead pieces per thread of a row; logits and gradient lie at the same distance from 16-byte boundaries.
-constexpr int kGradAhead = 4;
+constexpr int kGradAhead = 2;
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(mca_token_logprobs_backward_args a,
@@ -709,11 +716,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(mca_token_l
   const int j0 = (int)(blockIdx.x - r * parts) * kThreads * kGradAhead + threadIdx.x;
   const P row(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld, a.vocab);
   elem_t<DT>* out = static_cast<elem_t<DT>*>(a.grad) + r * a.ldg;
-  const Grad g(a, r);
   uint4 q[kGradAhead];
 #pragma unroll
   for (int i = 0; i < kGradAhead; ++i)
     if (j0 + i * kThreads < row.count && row.whole(j0 + i * kThreads)) q[i] = row.raw(j0 + i * kThreads);
+  const Grad g(a, r);
 #pragma unroll
   for (int i = 0; i < kGradAhead; ++i) {
     const int j = j0 + i * kThreads;
