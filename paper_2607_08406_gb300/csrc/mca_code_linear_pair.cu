@@ -11,6 +11,10 @@
 // Bulk copies bring chunks (16 KB of each operand) into a ring of six stages. The sums have two places in tensor
 // memory (2 x 256 columns): while one is read, scaled and written, the next tile's MMAs run.
 //
+// 8192 x 8192 -> 8192: 590 us, 1.86 PFLOP/s with the conversion, the tensor cores 86 % busy. With few columns the operands'
+// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 270 us (outputs fp16), 206 of them MMAs at the measured
+// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 320 us).
+//
 // Warps: 0 copies, 1 issues MMAs (the pair's first CTA), 4-19 take the sums (each 32 outputs and a
 // quarter of the samples). Sums of more than 1024 columns are added up as integers in registers and returned to tensor memory as fp32,
 // from where the outputs are written in one loop.

@@ -11,6 +11,10 @@
 // A row's 16 codes lie in two units of 8 columns; four threads of a row and eight rows share a store's quarter. The
 // units' distance is a multiple of 128 bytes plus 16, so that a quarter (two rows by four units) meets every bank once.
 //
+// 8192 -> 8192 takes 39 us for 128 samples, 32 for 64: about 1 us for a CTA's stage of 16 KB of weights, which the
+// conversions (130 instructions for 16 rows of 128 columns), the hand-overs and the loads' latency share; an M = 128 MMA
+// takes 80 cycles even for 16 samples, so that the tensor cores would allow 25 bytes of weights per cycle and SM.
+//
 // Each CTA of a cluster takes a part of the columns; the sums meet as integers in shared memory, where every CTA of
 // the cluster adds up and writes its share of the samples (their order cannot change a result).
 //
