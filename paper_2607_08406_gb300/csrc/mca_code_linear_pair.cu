@@ -39,7 +39,8 @@ constexpr int kStages = 6;
 constexpr uint32_t kChunk = kM * kSubK * 2;     // bytes of a block's chunk of 64 columns
 constexpr uint32_t kStage = 2 * kChunk;
 constexpr uint32_t kPairSmem = kStages * kStage + 1024;
-constexpr int kGroup = 8;                       // tiles of outputs that are taken together
+constexpr int kGroup = 8;                       // tiles of outputs that are taken together: so many at least,
+constexpr size_t kGroupBytes = 32 << 20;        //   and all whose weights are in so many bytes of L2
 constexpr uint32_t kIdesc = tc_idesc_f16(2 * kM, kT);
 
 struct PairArgs {
@@ -48,6 +49,7 @@ struct PairArgs {
   const unsigned char* ximg;
   int chunks;                                   // of 64 columns
   int nt_out, nt_rows;                          // tiles
+  int group;                                    // tiles of outputs that are taken together
 };
 
 // Rows' codes as fp16 in chunks of kM rows by 64 columns. A thread: a row's 64 columns (behind the last column
@@ -142,12 +144,12 @@ __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity) {
   }
 }
 
-// Tile of place i in the order of work: kGroup tiles of outputs at a time, for all samples, so that the pairs at
+// Tile of place i in the order of work: some tiles of outputs at a time, for all samples, so that the pairs at
 // work share their operands in L2.
 __device__ __forceinline__ void tile_at(const PairArgs& p, int i, int* n0, int64_t* r0) {
-  const int per = kGroup * p.nt_rows, g = i / per, k = i - g * per;
-  const int gn = min(kGroup, p.nt_out - g * kGroup);
-  *n0 = (g * kGroup + k % gn) * 2 * kM;
+  const int per = p.group * p.nt_rows, g = i / per, k = i - g * per;
+  const int gn = min(p.group, p.nt_out - g * p.group);
+  *n0 = (g * p.group + k % gn) * 2 * kM;
   *r0 = (int64_t)(k / gn) * kT;
 }
 
@@ -374,6 +376,7 @@ cudaError_t launch_code_linear_pair(const mca_code_linear_args& a, cudaStream_t 
   p.chunks = (a.n_in + kSubK - 1) / kSubK;
   p.nt_out = (int)tiles_of(a.n_out);
   p.nt_rows = (int)tiles_of(a.rows);
+  p.group = (int)std::min<size_t>(p.nt_out, std::max<size_t>(kGroup, kGroupBytes / (2 * (size_t)p.chunks * kChunk)));
   unsigned char* ws = static_cast<unsigned char*>(a.workspace);
   p.wimg = ws;
   p.ximg = ws + image_bytes(a.n_out, a.n_in);

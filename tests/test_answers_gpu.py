@@ -509,7 +509,7 @@ def answers(gpu_lib, x, w, ws, t, stream=None):
 
 
 @pytest.mark.parametrize("rows,n_in,vocab,ldw", [(1, 256, 1000, 256), (33, 100, 65, 100),
-                                                 (300, 512, 3001, 512)])
+                                                 (300, 512, 3001, 512), (2000, 512, 3001, 512)])
 def test_stream_and_graph(gpu_lib, rows, n_in, vocab, ldw):
     """The chain on another stream, captured and replayed on new inputs: bit for bit the eager results."""
     import torch
