@@ -74,6 +74,7 @@ mca_status check_pointers(mca_handle* h, const Arg (&args)[N]) {
 }
 
 constexpr int64_t kMaxRows = 0x7fffffff;     // rows of a call: a CTA each at least
+constexpr int kMaxIn = 131071;               // codes of a sum: 128 * 128 * kMaxIn < 2^31
 
 mca_status check_rows(mca_handle* h, int64_t rows) {
   if (rows < 0 || rows > kMaxRows)
@@ -115,8 +116,8 @@ bool overlap(const void* p, size_t np, const void* q, size_t nq) {
 mca_status check_linear(const mca_code_linear_args* a) {
   if (!a) return fail(nullptr, MCA_ERR_INVALID, "NULL argument");
   MCA_CHECK(check_rows(nullptr, a->rows));
-  if (a->n_in < 1 || a->n_in > 131071)
-    return fail(nullptr, MCA_ERR_INVALID, "n_in = %d outside 1..131071", a->n_in);
+  if (a->n_in < 1 || a->n_in > kMaxIn)
+    return fail(nullptr, MCA_ERR_INVALID, "n_in = %d outside 1..%d", a->n_in, kMaxIn);
   if (a->n_out < 1 || a->n_out > 1 << 30)
     return fail(nullptr, MCA_ERR_INVALID, "n_out = %d outside 1..2^30", a->n_out);
   MCA_CHECK(check_dtype(a->dtype));
@@ -274,6 +275,10 @@ bool bounded_by_one(const mca_layer& L) {
 mca_status check_predict(mca_handle* h, int64_t n) {
   if (!h) return fail(nullptr, MCA_ERR_INVALID, "NULL handle");
   if (h->tfm) return fail(h, MCA_ERR_UNSUPPORTED, "answers in 8-bit layers are for MLP handles");
+  for (const mca_layer& L : h->layers)
+    if (L.n_in > kMaxIn || L.n_out > 1 << 30)
+      return fail(h, MCA_ERR_UNSUPPORTED, "a layer of %d inputs and %d outputs: more than %d and 2^30 in 8 bits",
+                  L.n_in, L.n_out, kMaxIn);
   return check_rows(h, n);
 }
 

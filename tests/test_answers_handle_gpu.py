@@ -176,3 +176,16 @@ def test_predict_refusals(gpu_lib):
         vocab=20, ctx=8, d_model=16, n_layer=1, n_head=2, d_ff=32))
     ht = gpu_lib.create_from_tfm_workload(tw)
     assert lib.mca_predict_workspace_size(ht.ptr, 3, ctypes.byref(n)) == gpu_lib.MCA_ERR_UNSUPPORTED
+
+
+def test_predict_refuses_inputs_beyond_exact_sums(gpu_lib):
+    """More inputs than an integer sum of 8-bit codes has room for: trained, but not answered in 8 bits."""
+    import torch
+    for dims in [(131072, 4, 3), (5, 131072, 3)]:
+        wl = net(np.random.default_rng(2), dims, "tanh", "identity", "softmax_ce", 20)
+        h = gpu_lib.create_from_workload(wl)
+        x = torch.ones(2, dims[0], device="cuda")
+        for call in (lambda: gpu_lib.mca_predict(h, x), lambda: gpu_lib.mca_predict_workspace_size(h, 2)):
+            with pytest.raises(gpu_lib.MCAError, match="131071"):
+                call()
+        assert np.isfinite(gpu_lib.mca_loss(h))
