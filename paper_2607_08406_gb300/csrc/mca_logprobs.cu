@@ -242,8 +242,8 @@ __device__ __forceinline__ unsigned int first_cta(const void* p) {      // the a
 }
 
 // A row's pass without special cases: what lies below `low` counts as low (-inf too), whose terms vanish beside a
-// largest logit above `high`. Rows without one, or with less than the asked alternatives above low, go through
-// exact_row instead.
+// largest logit above `high`. Rows without one go through exact_row instead; alternatives that are not above low
+// come from rest_of_top.
 template <int DT>
 struct Range {
   static constexpr float low = DT == MCA_DTYPE_FP16 ? -65504.0f : -0x1p100f;
@@ -373,41 +373,6 @@ __device__ __forceinline__ Sums team_sums(Sums t, Team<W>& s) {
   return t;
 }
 
-// Any row, by the definition: passes for the largest logit, for the sums and for every alternative.
-template <int DT, int W>
-__device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>& s) {
-  const mca_token_logprobs_args& a = p.a;
-  const elem_t<DT>* x = static_cast<const elem_t<DT>*>(a.logits) + r * a.ld;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  Sums t{kLowest, 0.0f, 0.0f};
-  for (int v = tid; v < a.vocab; v += 32 * W) t.m = fmaxf(t.m, elem_f32(x[v]));
-  for (int v = tid; v < a.vocab; v += 32 * W) t.add(elem_f32(x[v]));
-  __syncwarp();
-  team_sync<W>();
-  t = team_sums<W>(t, s);
-  if (tid == 0) write_row<DT>(p, r, x, t);
-  const Row w(t);
-  Key last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    Key best = 0ull;
-    if (last > 1ull)
-      for (int v = tid; v < a.vocab; v += 32 * W) {
-        const Key q = order_key(elem_f32(x[v]), v);
-        if (q < last && q > best) best = q;
-      }
-    __syncwarp();
-    best = warp_max(best);
-    if constexpr (W > 1) {
-      team_sync<W>();
-      if (lane == 0) s.key[warp] = best;
-      team_sync<W>();
-      for (int q = 0; q < W; ++q) best = s.key[q] > best ? s.key[q] : best;
-    }
-    if (tid == 0) write_top(a, r, k, best, w);
-    last = best ? best : 1ull;
-  }
-}
-
 // The candidates: the logits that reach the bound, which lie in the groups whose largest does. Their pieces are read again
 // by the whole CTA, all at once. A thread's group g holds its pieces g size .. of the order that it took them in.
 template <int DT, int W>
@@ -450,10 +415,49 @@ __device__ __forceinline__ Key exchange(Key k, int j, bool larger) {
   return (q > k) == larger ? q : k;
 }
 
+// Lists of the n <= 32 largest keys, a key per lane in falling order: q of every lane into it. What lies behind the n-th is
+// one of the keys, and not looked at.
+__device__ __forceinline__ void keep_largest(Key& mine, Key q, int n) {
+  const int lane = threadIdx.x & 31;
+  unsigned int found = __ballot_sync(0xffffffffu, q > __shfl_sync(0xffffffffu, mine, n - 1));
+  while (found) {
+    const int from = __ffs(found) - 1;
+    const Key f = __shfl_sync(0xffffffffu, q, from);
+    const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
+    if (mine < f) mine = lane == 0 || above > f ? f : above;
+    found &= ~(1u << from);
+    found &= __ballot_sync(0xffffffffu, q > __shfl_sync(0xffffffffu, mine, n - 1));
+  }
+}
+
+// The warps' lists into one at s.cand, of s.n keys.
+template <int W>
+__device__ __forceinline__ void merge_lists(Key mine, Team<W>& s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncwarp();
+  team_sync<W>();                            // the candidates' places are free
+  s.cand[warp * 32 + lane] = mine;
+  for (int n = W / 2; n > 0; n >>= 1) {
+    team_sync<W>();
+    if (warp < n) {
+      const Key q = s.cand[(warp + n) * 32 + 31 - lane];
+      mine = q > mine ? q : mine;
+#pragma unroll
+      for (int j = 16; j > 0; j >>= 1) mine = exchange(mine, j, (lane & j) == 0);
+    }
+    if (warp < n) s.cand[warp * 32 + lane] = mine;
+  }
+  const int have = __popc(__ballot_sync(0xffffffffu, mine != 0ull));
+  if (warp == 0 && lane == 0) s.n = have;
+  __syncwarp();
+  team_sync<W>();
+}
+
 // The alternatives where the candidates are too many (logits in falling order, or many equal ones): each warp keeps the
-// 32 largest in order, a list per warp at s.cand, which are then merged in pairs. Returns how many there are.
+// n largest in order, a list per warp at s.cand, which are then merged in pairs.
 template <int DT, int W>
-__device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, Key key, Key bound, Team<W>& s) {
+__device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, int n, Key key, Key bound,
+                                         Team<W>& s) {
   constexpr int N = Pieces<DT>::N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Key mine = 0ull;
@@ -472,34 +476,90 @@ __device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, 
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const Key q = v[i] > Range<DT>::low ? order_key(v[i], row.index(j, i)) : 0ull;
-        const Key last = __shfl_sync(0xffffffffu, mine, 31);
-        unsigned int found = __ballot_sync(0xffffffffu, q > last && q >= bound);
-        while (found) {
-          const Key f = __shfl_sync(0xffffffffu, q, __ffs(found) - 1);
-          found &= found - 1;
-          const Key above = __shfl_up_sync(0xffffffffu, mine, 1);
-          if (mine < f) mine = lane == 0 || above > f ? f : above;
-        }
+        keep_largest(mine, q >= bound ? q : 0ull, n);
+      }
+    }
+  }
+  merge_lists<W>(mine, s);
+}
+
+// The largest n of a row's logits up to `limit`, in order, and how many they are at s.cand and s.n. A warp's pieces lie in
+// the order of their index: of equal logits, as a mask leaves them, the first are kept and the others end at the vote.
+template <int DT, int W>
+__device__ __noinline__ void rest_of_top(const Pieces<DT>& row, float limit, int n, Team<W>& s) {
+  constexpr int N = Pieces<DT>::N, kStep = 32 * W, kBatch = 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Key mine = 0ull;
+  for (int b = warp * 32; b < row.count; b += kBatch * kStep) {
+    uint4 q[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (b + i * kStep + lane < row.count) q[i] = row.bits(b + i * kStep + lane);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = b + i * kStep + lane;
+      float v[N], m = -INFINITY;
+      Pieces<DT>::values(q[i], v);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        v[k] = j < row.count && v[k] <= limit ? v[k] : -INFINITY;
+        m = fmaxf(m, v[k]);
+      }
+      __syncwarp();
+      const Key last = __shfl_sync(0xffffffffu, mine, n - 1);
+      if (!__any_sync(0xffffffffu, order_key(m, max(row.index(j, 0), 0)) > last)) continue;
+#pragma unroll
+      for (int k = 0; k < N; ++k) keep_largest(mine, order_key(v[k], row.index(j, k)), n);
+    }
+  }
+  merge_lists<W>(mine, s);
+}
+
+// Any row, by the definition: passes for the largest logit, and, unless that says it all, for the sums and the alternatives.
+template <int DT, int W>
+__device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, const Pieces<DT>& row, Team<W>& s) {
+  const mca_token_logprobs_args& a = p.a;
+  constexpr int N = Pieces<DT>::N, kStep = 32 * W, kBatch = 4;
+  float top = -INFINITY;                    // NaN if one is
+  for (int b = threadIdx.x; b < row.count; b += kBatch * kStep) {
+    uint4 q[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (b + i * kStep < row.count) q[i] = row.bits(b + i * kStep);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      float v[N];
+      Pieces<DT>::values(q[i], v);
+      if (b + i * kStep < row.count) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = max_nan(top, v[k]);
       }
     }
   }
   __syncwarp();
-  team_sync<W>();                            // the candidates' places are free
-  s.cand[warp * 32 + lane] = mine;
-  for (int n = W / 2; n > 0; n >>= 1) {
-    team_sync<W>();
-    if (warp < n) {
-      const Key q = s.cand[(warp + n) * 32 + 31 - lane];
-      mine = q > mine ? q : mine;
 #pragma unroll
-      for (int j = 16; j > 0; j >>= 1) mine = exchange(mine, j, (lane & j) == 0);
-    }
-    if (warp < n) s.cand[warp * 32 + lane] = mine;
-  }
-  const int have = __popc(__ballot_sync(0xffffffffu, mine != 0ull));
-  if (warp == 0 && lane == 0) s.n = have;
-  __syncwarp();
+  for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   team_sync<W>();
+  // the row's largest, with a sum of 0 where all are -inf and NaN where one is NaN or +inf
+  Sums t = team_sums<W>({fmaxf(top, kLowest), top < INFINITY ? (top > -INFINITY ? 1.0f : 0.0f) : NAN, 0.0f}, s);
+  const bool any = t.s > 0.0f;
+  if (any) {
+    t.s = t.u = 0.0f;
+#pragma unroll 2
+    for (int j = threadIdx.x; j < row.count; j += kStep) {
+      float v[N];
+      row.load(j, v);
+#pragma unroll
+      for (int k = 0; k < N; ++k) t.add(v[k]);
+    }
+    __syncwarp();
+    team_sync<W>();
+    t = team_sums<W>(t, s);
+  }
+  if (threadIdx.x == 0) write_row<DT>(p, r, row.x, t);
+  const Row w(t);
+  if (a.top > 0 && any) rest_of_top<DT, W>(row, INFINITY, a.top, s);
+  for (int k = threadIdx.x; k < a.top; k += kStep) write_top(a, r, k, any && k < s.n ? s.cand[k] : 0ull, w);
 }
 
 // Of n candidates the a.top largest, each at its place: put(place, key).
@@ -610,7 +670,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
     find_candidates<DT, W>(row, j0, j1, size, seen.top, bound, s);
     __syncwarp();
     team_sync<W>();
-    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row, j0, j1, key, bound, s);
+    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row, j0, j1, a.top, key, bound, s);
   }
 
   const Key* cand = s.cand;
@@ -642,10 +702,10 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
     found = 0;
     for (int q = 0; q < n; q += 32) found += __popc(__ballot_sync(0xffffffffu, q + lane < n && s_best[q + lane] != 0ull));
   }
-  if (t.m <= Range<DT>::high || (found < a.top && !w.bad)) {
+  if (t.m <= Range<DT>::high) {
     __syncwarp();
     team_sync<W>();
-    exact_row<DT, W>(p, r, s);
+    exact_row<DT, W>(p, r, row, s);
     return;
   }
   if (tid == 0) write_row<DT>(p, r, row.x, t);
@@ -656,6 +716,12 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
   place_top<W>(cand, n, a.top, [&](int at, Key k) {
     if (k != 0ull) write_top(a, r, at, k, w);
   });
+  if (found < a.top) {                                            // all above low are placed: those below
+    __syncwarp();
+    team_sync<W>();
+    rest_of_top<DT, W>(row, Range<DT>::low, a.top - found, s);
+    for (int k = found + tid; k < a.top; k += kTeam) write_top(a, r, k, k - found < s.n ? s.cand[k - found] : 0ull, w);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------

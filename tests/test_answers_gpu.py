@@ -398,6 +398,27 @@ def test_many_rows_in_any_order(gpu_lib, vocab, top):
     check_logprobs(gpu_lib, x, rng.integers(0, vocab, 1030), top, "float32")
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("rows,vocab,top", [(3, 70001, 32), (170, 9001, 20), (700, 4099, 32), (3000, 1200, 8)])
+def test_fewer_symbols_than_alternatives(gpu_lib, rows, vocab, top, dtype):
+    """Masks that leave less symbols than are asked for, with -inf, the type's lowest value, both of them, or
+    falling values near it behind; at the row's ends, side by side, anywhere."""
+    import torch
+    rng = np.random.default_rng(rows + top)
+    low = float(torch.finfo(torch_dtype(dtype)).min)
+    x = rng.standard_normal((rows, vocab))
+    for r in range(min(rows, 60)):
+        left = rng.choice(vocab, r % (top + 2), replace=False) if r % 3 else np.arange(r % top)
+        v = x[r, left]
+        x[r] = [-np.inf, low, low][r // 3 % 3]
+        if r // 3 % 3 == 2:
+            x[r, rng.random(vocab) < 0.9] = -np.inf
+        if r % 7 == 6 and dtype != "float16":
+            x[r] = -2e36 - 1e33 * (np.arange(vocab) // 3) * rng.choice([-0.01, 1.0])
+        x[r, left] = v
+    check_logprobs(gpu_lib, x, rng.integers(0, vocab, rows), top, dtype)
+
+
 def test_logprobs_of_shifted_rows(gpu_lib):
     """A common shift of a row's logits changes neither log probabilities nor entropy: differences are taken
     before exponentials."""
