@@ -78,7 +78,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs& p, int64_t r, const
   if (a.lse) a.lse[r] = w.bad ? NAN : w.none ? -INFINITY : w.m + w.ls;
   if (a.entropy) a.entropy[r] = w.bad ? NAN : w.none ? 0.0f : w.ls - t.u / t.s;
   if (a.logprob) {
-    const int y = a.targets[r / p.period * p.pitch + r % p.period];
+    const int y = a.targets[p.pitch == 0 ? r : r / p.period * p.pitch + r % p.period];
     float lp = 0.0f;
     if (y != -1)
       lp = y < 0 || y >= a.vocab || w.bad ? NAN : w.none ? -INFINITY : w.logprob(elem_f32(x[y]));
@@ -204,18 +204,15 @@ struct Pieces {
   }
   // Any piece of the row, -inf in the place of what is outside.
   __device__ __forceinline__ uint4 bits(int j) const {
-    return whole(j) ? raw(j) : part(j);
+    return whole(j) ? raw(j) : part(x, V, index(j, 0));
   }
-  __device__ __noinline__ uint4 part(int j) const {
+  __device__ __noinline__ static uint4 part(const elem_t<DT>* x, int V, int at) {
     union {
       elem_t<DT> e[N];
       uint4 u;
     } o;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int q = index(j, i);
-      o.e[i] = q >= 0 && q < V ? x[q] : elem_of<DT>(-INFINITY);
-    }
+    for (int i = 0; i < N; ++i) o.e[i] = at + i >= 0 && at + i < V ? x[at + i] : elem_of<DT>(-INFINITY);
     return o.u;
   }
   __device__ __forceinline__ void load(int j, float (&v)[N]) const { values(bits(j), v); }
@@ -456,8 +453,9 @@ __device__ __forceinline__ void merge_lists(Key mine, Team<W>& s) {
 // The alternatives where the candidates are too many (logits in falling order, or many equal ones): each warp keeps the
 // n largest in order, a list per warp at s.cand, which are then merged in pairs.
 template <int DT, int W>
-__device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, int n, Key key, Key bound,
+__device__ __noinline__ void ordered_top(const elem_t<DT>* x, int V, int j0, int j1, int n, Key key, Key bound,
                                          Team<W>& s) {
+  const Pieces<DT> row(x, V);
   constexpr int N = Pieces<DT>::N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Key mine = 0ull;
@@ -486,7 +484,8 @@ __device__ __noinline__ void ordered_top(const Pieces<DT>& row, int j0, int j1, 
 // The largest n of a row's logits up to `limit`, in order, and how many they are at s.cand and s.n. A warp's pieces lie in
 // the order of their index: of equal logits, as a mask leaves them, the first are kept and the others end at the vote.
 template <int DT, int W>
-__device__ __noinline__ void rest_of_top(const Pieces<DT>& row, float limit, int n, Team<W>& s) {
+__device__ __noinline__ void rest_of_top(const elem_t<DT>* x, int V, float limit, int n, Team<W>& s) {
+  const Pieces<DT> row(x, V);
   constexpr int N = Pieces<DT>::N, kStep = 32 * W, kBatch = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Key mine = 0ull;
@@ -517,8 +516,9 @@ __device__ __noinline__ void rest_of_top(const Pieces<DT>& row, float limit, int
 
 // Any row, by the definition: passes for the largest logit, and, unless that says it all, for the sums and the alternatives.
 template <int DT, int W>
-__device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, const Pieces<DT>& row, Team<W>& s) {
+__device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>& s) {
   const mca_token_logprobs_args& a = p.a;
+  const Pieces<DT> row(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld, a.vocab);
   constexpr int N = Pieces<DT>::N, kStep = 32 * W, kBatch = 4;
   float top = -INFINITY;                    // NaN if one is
   for (int b = threadIdx.x; b < row.count; b += kBatch * kStep) {
@@ -558,7 +558,7 @@ __device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, const Pi
   }
   if (threadIdx.x == 0) write_row<DT>(p, r, row.x, t);
   const Row w(t);
-  if (a.top > 0 && any) rest_of_top<DT, W>(row, INFINITY, a.top, s);
+  if (a.top > 0 && any) rest_of_top<DT, W>(row.x, row.V, INFINITY, a.top, s);
   for (int k = threadIdx.x; k < a.top; k += kStep) write_top(a, r, k, any && k < s.n ? s.cand[k] : 0ull, w);
 }
 
@@ -575,7 +575,7 @@ __device__ __forceinline__ void place_top(const Key* cand, int n, int top, Put p
 }
 
 template <int DT, int W>
-__global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(LogprobArgs p, int split) {
+__global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p, int split) {
   using P = Pieces<DT>;
   constexpr int kTeam = 32 * W;
   __shared__ Team<W> s;
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
         if ((unsigned int)(next - w0) < (unsigned int)whole) {
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot), "l"(x) : "memory");
         } else {
-          const uint4 q = row.part(next);
+          const uint4 q = P::part(row.x, row.V, row.index(next, 0));
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
                        ::"r"(slot), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
         }
@@ -670,7 +670,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
     find_candidates<DT, W>(row, j0, j1, size, seen.top, bound, s);
     __syncwarp();
     team_sync<W>();
-    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row, j0, j1, a.top, key, bound, s);
+    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row.x, row.V, j0, j1, a.top, key, bound, s);
   }
 
   const Key* cand = s.cand;
@@ -705,7 +705,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
   if (t.m <= Range<DT>::high) {
     __syncwarp();
     team_sync<W>();
-    exact_row<DT, W>(p, r, row, s);
+    exact_row<DT, W>(p, r, s);
     return;
   }
   if (tid == 0) write_row<DT>(p, r, row.x, t);
@@ -719,7 +719,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 32 : 40 / W) logprobs_kernel(
   if (found < a.top) {                                            // all above low are placed: those below
     __syncwarp();
     team_sync<W>();
-    rest_of_top<DT, W>(row, Range<DT>::low, a.top - found, s);
+    rest_of_top<DT, W>(row.x, row.V, Range<DT>::low, a.top - found, s);
     for (int k = found + tid; k < a.top; k += kTeam) write_top(a, r, k, k - found < s.n ? s.cand[k - found] : 0ull, w);
   }
 }
