@@ -5,7 +5,7 @@
 // with c the change of m, s becomes f s and u becomes f (u + s c), f = exp(c). Differences are taken before anything
 // is scaled, so that a common shift of a row loses nothing. Both kernels read every logit once; the gradient is a
 // product per logit. The least they take is the memory's time, 30 us for 2048 x 50001 bf16 (0.2 GB at 6.8 TB/s). Measured
-// there: 43 us without alternatives, 51 with 8, and the gradient 69 of 60: some 100 instructions for 8 logits (160 of the
+// there: 43 us without alternatives, 51 with 8, and the gradient 67 of 60: some 100 instructions for 8 logits (160 of the
 // gradient) keep the schedulers 60 to 80 % busy, and rows end unevenly.
 //
 // Alternatives without a second pass: a thread keeps the largest logit of each of up to 8 groups of its 16-byte pieces. The
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kAhead = 4;                 // pieces that a thread has on their way (6: 53 us, 8: 54)
+constexpr int kAhead = 4;                 // pieces that a thread has on their way (51 us; 6: 53, 8: 54)
 constexpr int kGroups = 8;                // groups of a thread's pieces
 constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary
 
@@ -483,6 +483,7 @@ __device__ __noinline__ void ordered_top(const elem_t<DT>* x, int V, int j0, int
 
 // The largest n of a row's logits up to `limit`, in order, and how many they are at s.cand and s.n. A warp's pieces lie in
 // the order of their index: of equal logits, as a mask leaves them, the first are kept and the others end at the vote.
+// (2048 x 50001 bf16, 5 symbols left of 8 asked for: 104 us, where a pass for each alternative took 600.)
 template <int DT, int W>
 __device__ __noinline__ void rest_of_top(const elem_t<DT>* x, int V, float limit, int n, Team<W>& s) {
   const Pieces<DT> row(x, V);
@@ -774,7 +775,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_small_kernel(mca_t
 }
 
 // kGradAhead pieces per thread of a row; logits and gradient lie at the same distance from 16-byte boundaries. (2048 x
-// 50001 bf16: 69 us with two, 72 with four; the 32 bytes of one thread side by side: 83.)
+// 50001 bf16: 66 us with two, 71 with four; the 32 bytes of one thread side by side took 83 when two took 69.)
 constexpr int kGradAhead = 2;
 
 template <int DT>
