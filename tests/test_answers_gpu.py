@@ -257,6 +257,30 @@ def test_code_linear_largest_sums_of_many(gpu_lib, rows, n_in, n_out, code):
     assert np.array_equal(got, s.astype(np.float32).astype(np.float64))
 
 
+@pytest.mark.parametrize("rows,n_out", [(7, 3001), (2500, 2), (40001, 45), (3001, 300)])
+@pytest.mark.parametrize("dtype", DT)
+def test_gelu_of_any_field(gpu_lib, rows, n_out, dtype):
+    """Fields over the whole range, which are the scales' products exactly, so that only the function is off: 18 + 1.5 z^2
+    half steps at most (the exponent's roundings grow with its size), tails below 2^-126 flushed."""
+    import torch
+    rng = np.random.default_rng(rows)
+    xs = np.concatenate([[0.0, 1e-30, 3e4, np.nan, np.inf], rng.uniform(0, 14, rows)])[:rows].astype(np.float32)
+    ws = np.concatenate([[1.0, -1.0], rng.uniform(-1, 1, n_out)])[:n_out].astype(np.float32)
+    with np.errstate(all="ignore"):
+        z = (xs[:, None] * ws).astype(np.float32).astype(np.float64)
+    one = np.ones((rows, 1), np.int8), np.ones((n_out, 1), np.int8)
+    got = run_linear(gpu_lib, *one, xs, ws, None, "gelu", 0.0, dtype)
+    assert np.isnan(got[np.isnan(z)]).all() and (got[z == np.inf] == np.inf).all() and (got[z == -np.inf] == 0).all()
+    fin = np.isfinite(z)
+    z, got = z[fin], got[fin]
+    want = R.act("gelu", z, 0.0)[0]
+    tol = 1.01 * R.U * (18 + 1.5 * np.minimum(z * z, 400.0)) * np.abs(want) + 20 * 2.0 ** -126
+    if dtype != "float32":
+        tol = tol + R.HALF_STEP[dtype] * (np.abs(want) + tol) + R.TINY[dtype]
+    assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
+    assert dtype == "float32" or torch.finfo(torch_dtype(dtype)).max > np.abs(want).max()
+
+
 def test_code_linear_scales(gpu_lib):
     """Scales of zero, tiny and huge magnitude, infinities and NaN go through by IEEE rules."""
     rng = np.random.default_rng(3)
