@@ -12,8 +12,10 @@
 // memory (2 x 256 columns): while one is read, scaled and written, the next tile's MMAs run.
 //
 // 8192 x 8192 -> 8192: 590 us, 1.86 PFLOP/s with the conversion, the tensor cores 86 % busy. With few columns the operands'
-// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 270 us (outputs fp16), 206 of them MMAs at the measured
-// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 320 us).
+// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 254 us (outputs fp16), 206 of them MMAs at the measured
+// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 306 us). With
+// fewer still it is the outputs' instructions, 11 a field and the function's: 14346 x 64 -> 15616 fp16 takes 147 us, Gaussian
+// 211, GELU 241 (66 are the outputs' way to memory).
 //
 // Warps: 0 copies, 1 issues MMAs (the pair's first CTA), 4-19 take the sums (each 32 outputs and a
 // quarter of the samples). Sums of more than 1024 columns are added up as integers in registers and returned to tensor memory as fp32,
@@ -159,7 +161,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_free[kStages], s_sum[2], s_taken[2];
   __shared__ uint32_t s_tmem;
-  __shared__ float s_scale[kSumWarps][kPart];   // of a tile's samples, for each warp that takes sums
+  __shared__ __align__(16) float s_scale[kSumWarps][kPart];   // of a tile's samples, for each warp that takes sums
   const mca_code_linear_args& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_rank();
@@ -316,9 +318,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         float v[16];
         if (ok) {
           tmem_ld16(from + (uint32_t)q, v);
-#pragma unroll
-          for (int k = 0; k < 16; ++k)
-            v[k] = code_field(v[k], xs[q + k], ws, b, a.bias != nullptr);
+          code_fields(v, reinterpret_cast<const float4*>(xs + q), ws, b, a.bias != nullptr);
           act_block(v, a.act, a.act_param);
         } else {
 #pragma unroll
