@@ -216,9 +216,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           bulk_chunk(to + kChunk, x + (size_t)c * kChunk, bar);
         }
       }
-      // copies in flight land before the CTA leaves
-      for (int q = at > kStages ? at - kStages : 0; q < at; ++q)
+      // Copies in flight land before the CTA leaves, and so do the arrivals of the MMAs that read them: they come from
+      // the first CTA, whose own have come when the second's may still be on their way.
+      for (int q = max(0, at - kStages); q < at; ++q)
         mbar_wait(&s_full[q % kStages], (uint32_t)(q / kStages) & 1u);
+      for (int q = max(0, at - kStages); q < at && ok; ++q)
+        ok = wait_pair(&s_free[q % kStages], (uint32_t)(q / kStages) & 1u);
     }
     __syncwarp();
   } else if (warp == 1) {
