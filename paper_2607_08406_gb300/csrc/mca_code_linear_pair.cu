@@ -8,22 +8,30 @@
 // of them issuing the conversions, against 896 cycles of MMAs) 8192 x 8192 -> 8192 took 965 us.
 //
 // Each CTA of a pair takes 128 of the outputs and half of the samples; the MMA reads both halves of the samples.
-// Bulk copies bring chunks (16 KB of each operand) into a ring of six stages. The sums have two places in tensor
+// Tensor copies bring chunks (16 KB of each operand) into a ring of six stages. The sums have two places in tensor
 // memory (2 x 256 columns): while one is read, scaled and written, the next tile's MMAs run.
 //
-// 8192 x 8192 -> 8192: 590 us, 1.86 PFLOP/s with the conversion, the tensor cores 86 % busy. With few columns the operands'
-// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 254 us (outputs fp16), 206 of them MMAs at the measured
-// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 306 us). With
-// fewer still it is the outputs' instructions, 11 a field and the function's: 14346 x 64 -> 15616 fp16 takes 147 us, Gaussian
-// 211, GELU 241 (66 are the outputs' way to memory).
+// The first CTA's MMAs read what both CTAs' copies brought: the copies of both (cta_group::2) count their bytes on the
+// first CTA's barrier, which orders them for the cluster. That the second CTA's sums have been read is passed on by one of
+// its threads, with the cluster's scope: an arrival of that scope takes 1200 cycles, which nothing waits for there (from
+// each warp that takes sums 14346 x 64 -> 15616 fp16 took 171 us, so
+// 157; with a thread that handed over each chunk 8192 x 8192 -> 8192 took 1600 us, so 600).
 //
-// Warps: 0 copies, 1 issues MMAs (the pair's first CTA), 4-19 take the sums (each 32 outputs and a
-// quarter of the samples). Sums of more than 1024 columns are added up as integers in registers and returned to tensor memory as fp32,
-// from where the outputs are written in one loop.
+// 8192 x 8192 -> 8192: 600 us, 1.83 PFLOP/s with the conversion, the tensor cores 86 % busy. With few columns the operands'
+// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 255 us (outputs fp16), 206 of them MMAs at the measured
+// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 313 us). With
+// fewer still it is the outputs' instructions, 11 a field and the function's: 14346 x 64 -> 15616 fp16 takes 157 us (66 are
+// the outputs' way to memory).
+//
+// Warps: 0 copies, 1 issues MMAs (in the pair's first CTA) or passes on that sums are read (in the second), 4-19 take
+// the sums (each 32 outputs and a quarter of the samples). Sums of more than 1024 columns are added up as integers in
+// registers and returned to tensor memory as fp32, from where the outputs are written in one loop.
 //
 // Every wait is bounded (2 s). After one that ran out the later ones do too, and the outputs not yet written
 // become NaN.
 #include <algorithm>
+
+#include <cuda.h>
 
 #include "mca_code_linear.cuh"
 
@@ -40,6 +48,8 @@ constexpr int kSubK = 64;                       // columns per chunk
 constexpr int kStages = 6;
 constexpr uint32_t kChunk = kM * kSubK * 2;     // bytes of a block's chunk of 64 columns
 constexpr uint32_t kStage = 2 * kChunk;
+// The images as a matrix of 32-bit words for the tensor copies: a chunk is a box of kBoxRows rows.
+constexpr uint32_t kBoxWords = 256, kBoxRows = kChunk / (4 * kBoxWords);
 constexpr uint32_t kPairSmem = kStages * kStage + 1024;
 constexpr int kGroup = 8;                       // tiles of outputs that are taken together: so many at least,
 constexpr size_t kGroupBytes = 32 << 20;        //   and all whose weights are in so many bytes of L2
@@ -47,8 +57,8 @@ constexpr uint32_t kIdesc = tc_idesc_f16(2 * kM, kT);
 
 struct PairArgs {
   mca_code_linear_args a;
-  const unsigned char* wimg;
-  const unsigned char* ximg;
+  CUtensorMap images;                           // of the weights, and behind them of the samples
+  int ximg;                                     // the samples' first chunk
   int chunks;                                   // of 64 columns
   int nt_out, nt_rows;                          // tiles
   int group;                                    // tiles of outputs that are taken together
@@ -108,23 +118,21 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
                "[%0], %1;"
                ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
-// Arrive on the first CTA's barrier. (What is handed over are operands that copies of the async proxy wrote, and
-// places in tensor memory, by the tcgen05 fences: the arrival itself releases no more than a CTA's writes. With
-// .release.cluster it takes 1250 cycles.)
-__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+// The first CTA's barrier.
+__device__ __forceinline__ uint32_t first_bar(uint64_t* bar) {
   uint32_t at;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(bar)));
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
+  return at;
 }
-__device__ __forceinline__ void warp_arrive_first(uint64_t* bar) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) arrive_first(bar);
-  __syncwarp();
+// Arrive there, with what this thread has seen.
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_bar(bar)) : "memory");
 }
-// One thread: a chunk into shared memory, completing its bytes on bar.
-__device__ __forceinline__ void bulk_chunk(uint32_t dst, const void* src, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(kChunk), "r"(bar) : "memory");
+// One thread: a chunk of the images into shared memory, completing its bytes on the first CTA's bar.
+__device__ __forceinline__ void copy_chunk(uint32_t dst, const CUtensorMap* images, int chunk, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+               "[%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(images), "r"(0), "r"(chunk * (int)kBoxRows), "r"(bar) : "memory");
 }
 // mbar_wait for arrivals of the other CTA.
 __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity) {
@@ -157,7 +165,7 @@ __device__ __forceinline__ void tile_at(const PairArgs& p, int i, int* n0, int64
 
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-    code_linear_pair_kernel(PairArgs p) {
+    code_linear_pair_kernel(const __grid_constant__ PairArgs p) {
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_free[kStages], s_sum[2], s_taken[2];
   __shared__ uint32_t s_tmem;
@@ -178,12 +186,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   }
   if (tid == 32) {
     for (int q = 0; q < kStages; ++q) {
-      mbar_init(&s_full[q], rank == 0 ? 2 : 1);   // the first CTA's: its own copies, and the other's arrival
+      mbar_init(&s_full[q], 1);                   // the first CTA's: the bytes of both
       mbar_init(&s_free[q], 1);
     }
     for (int q = 0; q < 2; ++q) {
       mbar_init(&s_sum[q], 1);
-      mbar_init(&s_taken[q], 2 * kSumWarps);      // of both CTAs
+      mbar_init(&s_taken[q], kSumWarps + (rank == 0 ? 1 : 0));   // and the second CTA's thread that passes it on
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -201,25 +209,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         int n0;
         int64_t r0;
         tile_at(p, i, &n0, &r0);
-        const unsigned char* w = p.wimg + (size_t)(n0 / kM + rank) * nch * kChunk;
-        const unsigned char* x = p.ximg + (size_t)(r0 / kTB + rank) * nch * kChunk;
+        const int w = (n0 / kM + rank) * nch, x = p.ximg + (int)(r0 / kTB + rank) * nch;
         for (int c = 0; c < nch; ++c, ++at) {
           const int st = at % kStages;
           if (at >= kStages && !wait_pair(&s_free[st], (uint32_t)(at / kStages - 1) & 1u)) {
             ok = false;
             break;
           }
-          const uint32_t bar = smem_u32(&s_full[st]), to = ring + (uint32_t)st * kStage;
-          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                       ::"r"(bar), "r"(kStage) : "memory");
-          bulk_chunk(to, w + (size_t)c * kChunk, bar);
-          bulk_chunk(to + kChunk, x + (size_t)c * kChunk, bar);
+          const uint32_t bar = first_bar(&s_full[st]), to = ring + (uint32_t)st * kStage;
+          if (rank == 0)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                         ::"r"(smem_u32(&s_full[st])), "r"(2 * kStage) : "memory");
+          copy_chunk(to, &p.images, w + c, bar);
+          copy_chunk(to + kChunk, &p.images, x + c, bar);
         }
       }
-      // Copies in flight land before the CTA leaves, and so do the arrivals of the MMAs that read them: they come from
-      // the first CTA, whose own have come when the second's may still be on their way.
-      for (int q = max(0, at - kStages); q < at; ++q)
-        mbar_wait(&s_full[q % kStages], (uint32_t)(q / kStages) & 1u);
+      // The arrivals of the MMAs that read the last copies come before the CTA leaves: they are issued by the first CTA,
+      // whose own have come when the second's may still be on their way. (A wait that ran out has given the copies in
+      // flight its 2 s.)
       for (int q = max(0, at - kStages); q < at && ok; ++q)
         ok = wait_pair(&s_free[q % kStages], (uint32_t)(q / kStages) & 1u);
     }
@@ -227,15 +234,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   } else if (warp == 1) {
     if (elect_one()) {
       bool ok = true;
-      int u = 0, d = 0;                         // chunks consumed, sums begun
+      int u = 0, d = 0;                         // chunks consumed, sums begun (or passed on)
       for (int i = first; i < tiles && ok; i += step) {
+        if (rank != 0) {
+          for (int m = 0; m < nsum && ok; ++m, ++d) {
+            ok = mbar_wait(&s_taken[d & 1], (uint32_t)(d >> 1) & 1u);
+            tc_fence_after();
+            tc_fence_before();
+            if (ok) arrive_first(&s_taken[d & 1]);
+          }
+          continue;
+        }
         for (int c = 0; c < nch && ok; ++c, ++u) {
           const int st = u % kStages, in = c % kPer;
-          if (rank != 0) {                      // this CTA's chunk has come: tell the first
-            ok = mbar_wait(&s_full[st], (uint32_t)(u / kStages) & 1u);
-            if (ok) arrive_first(&s_full[st]);
-            continue;
-          }
           if (in == 0 && d >= 2) ok = wait_pair(&s_taken[d & 1], (uint32_t)(d / 2 - 1) & 1u);
           ok = ok && wait_pair(&s_full[st], (uint32_t)(u / kStages) & 1u);
           if (!ok) break;
@@ -299,7 +310,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           }
           if (m + 1 < nsum) {
             tc_fence_before();
-            warp_arrive_first(&s_taken[d & 1]);
+            warp_arrive(&s_taken[d & 1]);
           }
         }
         if (ok) {
@@ -341,7 +352,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       }
       if (ok) {
         tc_fence_before();
-        warp_arrive_first(&s_taken[(d - 1) & 1]);
+        warp_arrive(&s_taken[(d - 1) & 1]);
       }
     }
   }
@@ -367,6 +378,25 @@ size_t image_bytes(int64_t rows, int n_in) {
   return (size_t)tiles_of(rows) * 2 * (size_t)((n_in + kSubK - 1) / kSubK) * kChunk;
 }
 
+// The images' n chunks as the tensor copies see them; the driver's function by its name, which needs no library to link.
+cudaError_t images_map(CUtensorMap* map, void* img, size_t n) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  void* f = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  const cudaError_t e =
+      cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+  if (e != cudaSuccess) return e;
+  if (found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  const cuuint64_t dim[2] = {kBoxWords, n * kBoxRows}, stride[1] = {4 * kBoxWords};
+  const cuuint32_t box[2] = {kBoxWords, kBoxRows}, every[2] = {1, 1};
+  const CUresult r = reinterpret_cast<Encode>(f)(
+      map, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, img, dim, stride, box, every, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 }  // namespace
 
 size_t code_linear_pair_workspace(const mca_code_linear_args& a) {
@@ -381,14 +411,15 @@ cudaError_t launch_code_linear_pair(const mca_code_linear_args& a, cudaStream_t 
   p.nt_rows = (int)tiles_of(a.rows);
   p.group = (int)std::min<size_t>(p.nt_out, std::max<size_t>(kGroup, kGroupBytes / (2 * (size_t)p.chunks * kChunk)));
   unsigned char* ws = static_cast<unsigned char*>(a.workspace);
-  p.wimg = ws;
-  p.ximg = ws + image_bytes(a.n_out, a.n_in);
+  unsigned char* xs = ws + image_bytes(a.n_out, a.n_in);
+  p.ximg = (int)(image_bytes(a.n_out, a.n_in) / kChunk);
+  cudaError_t e = images_map(&p.images, ws, code_linear_pair_workspace(a) / kChunk);
+  if (e != cudaSuccess) return e;
   const ImageArgs w{a.w, a.n_out, a.ldw, ws, code_rows_aligned(a.w, a.n_out, a.ldw)};
-  const ImageArgs x{a.x, a.rows, a.ldx, ws + image_bytes(a.n_out, a.n_in),
-                    code_rows_aligned(a.x, a.rows, a.ldx)};
+  const ImageArgs x{a.x, a.rows, a.ldx, xs, code_rows_aligned(a.x, a.rows, a.ldx)};
   const int64_t wb = (a.n_out + kM - 1) / kM, xb = (a.rows + kM - 1) / kM;
   code_image_kernel<<<(unsigned int)((wb + xb) * p.chunks), kM, 0, s>>>(w, x, wb, a.n_in, p.chunks);
-  const cudaError_t e = cudaGetLastError();
+  e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int pairs = (int)std::min<int64_t>(76, (int64_t)p.nt_out * p.nt_rows);
   switch (a.dtype) {
