@@ -423,7 +423,10 @@ def mca_selftest_wait_timeout():
 # ------------------------------------------------------------------------------------------------
 # A trained net's answers. Tensors are CUDA tensors of one device, matrices with unit column stride;
 # results are new tensors (or the ones given). Work is queued on `stream` (a torch.cuda.Stream or
-# cudaStream_t, default: the device's current torch stream), and tensors made here belong to it.
+# cudaStream_t, default: the device's current torch stream), and tensors made here belong to it. On
+# another stream than the current one the tensors given are recorded there, so that their memory is not
+# handed out again before the work is done; that they are ready is for the caller to see to
+# (stream.wait_stream), as for any other work on a stream.
 # ------------------------------------------------------------------------------------------------
 
 torch = None             # the module, once one of the calls below has needed it
@@ -486,8 +489,9 @@ def _dtype_code(dtype) -> int:
         raise ValueError(f"dtype {dtype}: expected float32, float16 or bfloat16") from None
 
 
-def _on(index, stream, call):
-    """call(stream's cudaStream_t) with device `index` current and tensors allocated on the stream."""
+def _on(index, stream, given, call):
+    """call(stream's cudaStream_t) with device `index` current and tensors allocated on the stream; the
+    tensors `given` (None: none) are recorded on it."""
     if stream is not None:
         stream = getattr(stream, "cuda_stream", stream)
     if torch._C._cuda_getDevice() == index:
@@ -497,15 +501,21 @@ def _on(index, stream, call):
     with torch.cuda.device(index):
         if stream is None or stream == torch.cuda.current_stream().cuda_stream:
             return call(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream
-                               else torch.cuda.default_stream()):
-            return call(stream)
+        st = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        try:
+            with torch.cuda.stream(st):
+                return call(stream)
+        finally:
+            for t in given:
+                if t is not None:
+                    t.record_stream(st)
 
 
 def mca_quantize_rows(x, codes=None, scale=None, stream=None):
     """Rows of x [rows, cols] in 8 bits: (codes [rows, cols] int8, scale [rows] float32), x ~ scale *
     codes. New codes' rows start on 16-byte boundaries (a view of a wider matrix when cols is not a
-    multiple of 16)."""
+    multiple of 16). stream, here and below: where the work is queued; the tensors have to be ready there
+    (stream.wait_stream), and their memory is kept until it is done."""
     _ready()
     rows, cols, ldx = _matrix("x", x, _dtypes)
     dev = x.get_device()
@@ -529,7 +539,7 @@ def mca_quantize_rows(x, codes=None, scale=None, stream=None):
                                         c.data_ptr(), ld, sc.data_ptr(), s))
         return c, sc
 
-    return _on(dev, stream, call)
+    return _on(dev, stream, (x, codes, scale), call)
 
 
 def _linear_args(x_codes, x_scale, w_codes, w_scale, bias, act, act_param, dtype):
@@ -593,7 +603,7 @@ def mca_code_linear(x_codes, x_scale, w_codes, w_scale, bias=None, act="identity
             _check(status)
         return y
 
-    return _on(dev, stream, call)
+    return _on(dev, stream, (x_codes, x_scale, w_codes, w_scale, bias, out, workspace), call)
 
 
 class TokenLogprobs(NamedTuple):
@@ -639,7 +649,7 @@ def mca_token_logprobs(logits, targets=None, top: int = 0, stream=None) -> Token
         _check(_fn["mca_token_logprobs"](ctypes.byref(a)))
         return r
 
-    return _on(dev, stream, call)
+    return _on(dev, stream, (logits, targets), call)
 
 
 def mca_token_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy=None, out=None,
@@ -669,7 +679,7 @@ def mca_token_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entr
         _check(_fn["mca_token_logprobs_backward"](ctypes.byref(a)))
         return g
 
-    return _on(dev, stream, call)
+    return _on(dev, stream, (logits, targets, lse, entropy, g_logprob, g_entropy, out), call)
 
 
 @contextmanager
@@ -683,11 +693,13 @@ def _handle_stream(h: Handle, *inputs):
     st = torch.cuda.ExternalStream(h.stream) if h.stream else torch.cuda.default_stream()
     st.wait_stream(cur)
     made = []
-    with torch.cuda.stream(st):
-        yield made
-    for t in inputs:
-        t.record_stream(st)
-    cur.wait_stream(st)
+    try:
+        with torch.cuda.stream(st):
+            yield made
+    finally:
+        for t in inputs:
+            t.record_stream(st)
+        cur.wait_stream(st)
     for t in made:
         t.record_stream(cur)
 
