@@ -46,6 +46,8 @@ mca_status fail(mca_handle* h, mca_status st, const char* fmt, ...) {
     h->err = buf;
   else
     g_create_err = buf;
+  // what this call returns is not left for the next call's launch to find
+  if (st == MCA_ERR_CUDA || st == MCA_ERR_OOM) cudaGetLastError();
   return st;
 }
 

@@ -34,14 +34,15 @@ size_t mlp2_loop_smem_bytes(const Mlp2Args& a) {
 int mlp2_loop_max_grid(const Mlp2Args& a, int num_sms) {
   const LoopFn loop = pick_loop(a);
   const size_t smem = mlp2_loop_smem_bytes(a);
-  if (smem > 0 && cudaFuncSetAttribute((const void*)loop,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)smem) != cudaSuccess)
-    return 0;
   int occ = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, loop, kLoopThreads, smem) !=
-      cudaSuccess)
+  if ((smem > 0 && cudaFuncSetAttribute((const void*)loop,
+                                        cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        (int)smem) != cudaSuccess) ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, loop, kLoopThreads, smem) !=
+          cudaSuccess) {
+    cudaGetLastError();            // an answer here, not an error for the next launch to find
     return 0;
+  }
   return occ * num_sms;
 }
 

@@ -52,6 +52,7 @@ bool on_device(const void* p) {
 
 mca_status set_err(mca_handle* h, mca_status st, const std::string& msg) {
   h->err = msg;
+  if (st == MCA_ERR_CUDA) cudaGetLastError();     // returned here, and not by the next call's launch again
   return st;
 }
 
