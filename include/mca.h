@@ -467,11 +467,13 @@ typedef struct {
 mca_status mca_token_logprobs(const mca_token_logprobs_args* a);
 
 /* The gradient of g_logprob[r] * logprob[r] + g_entropy[r] * entropy[r], summed over rows, with respect to
- * the logits: grad[r, v] = g_logprob ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy), with p_v = exp(logits[r, v] - lse[r]) from the
- * forward call's lse and entropy. Rows without a target (-1) take no part of g_logprob, with another target
- * outside [0, vocab) their gradient is NaN; rows whose logits are all -inf have gradient 0. A nullable array that is NULL counts as zeros (g_entropy and entropy go together, g_logprob and
- * targets too; not both pairs NULL). grad: [rows x vocab] of `dtype`; it may be `logits` itself with the same
- * ld, and overlaps it in no other way. */
+ * the logits: grad[r, v] = g_logprob ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy), with
+ * p_v = exp(logits[r, v] - lse[r]) from the forward call's lse and entropy. Rows without a target (-1) take
+ * no part of g_logprob, with another target outside [0, vocab) their gradient is NaN; rows whose logits are
+ * all -inf have gradient 0. A nullable array that is NULL counts as zeros (g_entropy and entropy go
+ * together, g_logprob and targets too; not both pairs NULL). grad: [rows x vocab] of `dtype`; it may be
+ * `logits` itself with the same ld, and shares no element with it otherwise (rows that lie between each
+ * other's, as of two halves of one wider matrix: with one ld only). */
 typedef struct {
   const void* logits;
   int32_t dtype;

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 
 #include <nvtx3/nvToolsExt.h>
 
@@ -111,6 +112,16 @@ size_t span_bytes(int64_t rows, int64_t cols, int64_t ld, size_t es) {
 bool overlap(const void* p, size_t np, const void* q, size_t nq) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return a < b + nq && b < a + np;
+}
+
+// The same for two matrices of one row distance: their rows may lie between each other's. Row i of the second starts
+// delta + (i - j) ld bytes behind row j of the first, and only the two multiples of ld next to -delta can bring it near.
+bool rows_overlap(const void* p, const void* q, int64_t rows, int64_t cols, int64_t ld, size_t es) {
+  const int64_t delta = (int64_t)(reinterpret_cast<uintptr_t>(q) - reinterpret_cast<uintptr_t>(p));
+  const int64_t width = cols * (int64_t)es, step = ld * (int64_t)es;
+  for (int64_t k = delta / step - 1; k <= delta / step + 1; ++k)
+    if (k > -rows && k < rows && std::llabs(delta - k * step) < width) return true;
+  return false;
 }
 
 mca_status check_linear(const mca_code_linear_args* a) {
@@ -364,9 +375,11 @@ mca_status mca_token_logprobs_backward(const mca_token_logprobs_backward_args* a
                                      {"g_logprob", a->g_logprob, 4, true},
                                      {"g_entropy", a->g_entropy, 4, true},
                                      {"grad", a->grad, es, false}}));
-  const bool same = a->grad == a->logits && (a->rows == 1 || a->ld == a->ldg);
-  if (!same && overlap(a->logits, span_bytes(a->rows, a->vocab, a->ld, es), a->grad,
-                       span_bytes(a->rows, a->vocab, a->ldg, es)))
+  const int64_t ld = a->rows > 1 ? a->ld : a->vocab, ldg = a->rows > 1 ? a->ldg : a->vocab;
+  if (!(a->grad == a->logits && ld == ldg) &&
+      overlap(a->logits, span_bytes(a->rows, a->vocab, ld, es), a->grad,
+              span_bytes(a->rows, a->vocab, ldg, es)) &&
+      (ld != ldg || rows_overlap(a->logits, a->grad, a->rows, a->vocab, ld, es)))
     return fail(nullptr, MCA_ERR_INVALID, "grad overlaps the logits but is not the same matrix");
   return launched(nullptr, mca::launch_logprobs_backward(*a, (cudaStream_t)a->stream),
                   "mca_token_logprobs_backward");
