@@ -88,3 +88,22 @@ def test_rows_that_rise_all_the_way(gpu_lib, rows, warps, step):
     x = (np.arange(V) // 4 * np.float32(step)).astype(np.float32).astype(np.float64)
     base = np.stack([x, x - x.max(), x - 100.0])
     check(logits_of(gpu_lib, base, rows), base, rows, chain(V, warps))
+
+
+def group_chain(V, warps, per_piece):
+    """The same where a thread's pieces come in eight groups, whose sums are added."""
+    pieces = -(-(V // per_piece + 2) // (32 * warps))
+    return per_piece // 2 * -(-pieces // 8) + 1 + 8 * 6
+
+
+@pytest.mark.parametrize("rows,warps,V", [(2433, 1, 160003), (2433, 1, 33001), (1300, 2, 120001), (700, 4, 80001)])
+def test_long_rows_of_few_values(gpu_lib, rows, warps, V):
+    """Few largest logits and a common value below them, whose roundings have one sign: they may add up over a thread's
+    group of pieces, not over all of them."""
+    base = []
+    for v in (-0.2613, -2.3005, -2.3203, -3.6999, -1.226, -0.7):
+        x = np.full(V, np.float32(v), np.float32).astype(np.float64)
+        x[:132 * warps] = 0.0                     # every thread has one
+        base.append(x)
+    base.append(np.where(np.arange(V) % 3, 0.0, np.float32(-0.7).astype(np.float64)))
+    check(logits_of(gpu_lib, np.stack(base), rows), np.stack(base), rows, group_chain(V, warps, 4))
