@@ -5,13 +5,13 @@
 // f (u + s c), f = exp(c). (m may lag behind by up to kLead, which see.) Differences are taken before anything
 // is scaled, so that a common shift of a row loses nothing. Both kernels read every logit once; the gradient is a
 // product per logit. The least they take is the memory's time, 30 us for 2048 x 50001 bf16 (0.2 GB at 6.8 TB/s). Measured
-// there: 43 us without alternatives, 51 with 8, and the gradient 67 of 60: some 100 instructions for 8 logits (160 of the
+// there: 45 us without alternatives, 53 with 8, and the gradient 67 of 60: some 100 instructions for 8 logits (160 of the
 // gradient) keep the schedulers 60 to 80 % busy, and rows end unevenly.
 //
-// Alternatives without a second pass: a thread keeps the largest logit of each of up to 8 groups of its 16-byte pieces. The
-// threads' largest give a bound that the k-th alternative cannot be below; few more than k groups reach it, and only
-// these are read again (from L2). What is found there is few enough to be put in order by counting. (Sorting the
-// threads' largest and merging lists over the CTA took 9 us of a row's 25.)
+// Alternatives without a second pass: a thread keeps the largest logit of each of up to 8 groups of its 16-byte pieces.
+// The k-th largest of a row's groups is a bound that the k-th alternative cannot be below; few more than k groups reach it
+// (no more, with one warp and no equal logits), and only these are read again (from L2). What is found there is few enough
+// to be put in order by counting. (Sorting the threads' largest and merging lists over the CTA took 9 us of a row's 25.)
 #include <algorithm>
 
 #include "mca_answers.h"
@@ -113,10 +113,6 @@ __device__ __forceinline__ unsigned int lanes_max(unsigned int v) {
     for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
   }
-}
-__device__ __forceinline__ Key warp_max(Key k) {
-  const unsigned int hi = lanes_max<32>((unsigned int)(k >> 32));
-  return (Key)hi << 32 | lanes_max<32>((unsigned int)(k >> 32) == hi ? (unsigned int)k : 0u);
 }
 
 template <int DT, int L, int N>
@@ -301,7 +297,6 @@ constexpr float kLead = 1.0f;
 template <int DT>
 struct Seen {
   float m = Range<DT>::low, top = Range<DT>::low;
-  int at = -1;                              // piece of the first logit of size top
   float2 s = {0.0f, 0.0f}, u = {0.0f, 0.0f};
   Sums all = {Range<DT>::low, 0.0f, 0.0f};  // of the groups before
   __device__ __forceinline__ void raise(float to) {
@@ -312,12 +307,11 @@ struct Seen {
     s.y *= f;
     m = to;
   }
-  __device__ __forceinline__ float take(const uint4& q, int j) {
+  __device__ __forceinline__ float take(const uint4& q) {
     float2 v[Pieces<DT>::N / 2];
     const float b = clamp_piece<DT>(q, v);
     if (b > top) {
       top = b;
-      at = j;
       if (b > m + kLead) raise(b);
     }
     const float2 mm = make_float2(-m, -m), l2 = make_float2(kLog2e, kLog2e);
@@ -355,7 +349,7 @@ struct Team {
   static constexpr int kCand = 64 * W;
   static_assert(kCand >= W * 32, "the lists of ordered_top");
   Sums sum[W];
-  Key key[W];
+  unsigned int bound[W];
   int n, flagged;                           // candidates; groups whose largest logit reaches the bound
   unsigned short flag[kGroups * 32 * W];    // their threads and numbers
   float top[kGroups][32 * W];               // largest logits of the threads' groups
@@ -468,14 +462,14 @@ __device__ __forceinline__ void merge_lists(Key mine, Team<W>& s) {
 // The alternatives where the candidates are too many (logits in falling order, or many equal ones): each warp keeps the
 // n largest in order, a list per warp at s.cand, which are then merged in pairs.
 template <int DT, int W>
-__device__ __noinline__ void ordered_top(const elem_t<DT>* x, int V, int j0, int j1, int n, Key key, Key bound,
+__device__ __noinline__ void ordered_top(const elem_t<DT>* x, int V, int j0, int j1, int n, float top, Key bound,
                                          Team<W>& s) {
   const Pieces<DT> row(x, V);
   constexpr int N = Pieces<DT>::N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Key mine = 0ull;
   // the warp takes its threads' pieces one thread after the other, a piece per lane
-  unsigned int todo = __ballot_sync(0xffffffffu, key != 0ull && key >= bound);
+  unsigned int todo = __ballot_sync(0xffffffffu, top > Range<DT>::low && order_key(top, 0) >= bound);
   while (todo) {
     const int owner = __ffs(todo) - 1;
     todo &= todo - 1;
@@ -646,7 +640,7 @@ __global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p,
       asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(slot) : "memory");
-      b = fmaxf(b, seen.take(q, j));
+      b = fmaxf(b, seen.take(q));
       if (--left == 0) {
         *group = b;
         seen.close();
@@ -666,31 +660,39 @@ __global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p,
 
   // the candidates: logits that reach the bound
   if (a.top > 0) {
-    Key key = 0ull;
-    if (seen.at >= 0) {
-      float v[P::N];
-      row.load(seen.at, v);
+    // a warp's k / W-th largest group, of equal ones all at once; k groups reach the smallest of the warps' (one thread's
+    // largest in place of each group's let through 130 logits for 32 alternatives and one warp, and half the row: 4096 x
+    // 32000 bf16 315 us, so 87; with 20 alternatives 86 and 76)
+    unsigned int v[kGroups], reach = 0u;
 #pragma unroll
-      for (int i = P::N - 1; i >= 0; --i)
-        if (v[i] == seen.top) key = order_key(seen.top, row.index(seen.at, i));
+    for (int g = 0; g < kGroups; ++g) {
+      const float b = j0 + g * size * kTeam + tid < j1 ? s.top[g][tid] : -INFINITY;
+      v[g] = b > Range<DT>::low ? (unsigned int)(order_key(b, 0) >> 32) : 0u;
     }
-    __syncwarp();
-    // k threads reach the smallest of the warps' k / W-th
-    Key bound = 0ull, rest = key;
-    for (int k = 0; k < (a.top + W - 1) / W; ++k) {
-      bound = warp_max(rest);
-      if (rest == bound) rest = 0ull;
+    for (int have = 0; have < (a.top + W - 1) / W;) {
+      unsigned int best = 0u, n = 0u;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) best = max(best, v[g]);
+      reach = best = lanes_max<32>(best);
+      if (best == 0u) break;                                    // no more groups: every candidate reaches 0
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        n += v[g] == best;
+        v[g] = v[g] == best ? 0u : v[g];
+      }
+      have += (int)__reduce_add_sync(0xffffffffu, n);
     }
     if constexpr (W > 1) {
-      if (lane == 0) s.key[warp] = bound;
+      if (lane == 0) s.bound[warp] = reach;
       team_sync<W>();
-      for (int q = 0; q < W; ++q) bound = s.key[q] < bound ? s.key[q] : bound;
+      for (int q = 0; q < W; ++q) reach = min(reach, s.bound[q]);
     }
+    const Key bound = (Key)reach << 32;
     __syncwarp();
     find_candidates<DT, W>(row, j0, j1, size, seen.top, bound, s);
     __syncwarp();
     team_sync<W>();
-    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row.x, row.V, j0, j1, a.top, key, bound, s);
+    if (s.n > Team<W>::kCand) ordered_top<DT, W>(row.x, row.V, j0, j1, a.top, seen.top, bound, s);
   }
 
   const Key* cand = s.cand;
