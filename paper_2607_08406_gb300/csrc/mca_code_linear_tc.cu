@@ -214,8 +214,15 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, T > 64 ? 1 : 2) code_linea
       ok = warp_all(mbar_wait(&s_free[c % kNC], (uint32_t)(c / kNC) & 1u));
     if (!ok) s_fail = 1;
   }
+  tc_fence_before();
   __syncwarp();
   __syncthreads();
+  // The sums are in shared memory. Tensor memory goes back before the CTA waits for others: a kernel that wants it on this
+  // SM may hold up one that the cluster's other CTAs wait for.
+  if (warp == S::kConvWarps) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kTmem));
+  }
   bool fail = s_fail != 0;
   if (p.splits > 1) {
     cluster_sync_all();
@@ -252,15 +259,7 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, T > 64 ? 1 : 2) code_linea
         if (t + i * step < nt) *y = elem_of<DT>(fail ? NAN : z[i]);
     }
   }
-  tc_fence_before();
-  if (p.splits > 1) {
-    cluster_sync_all();
-  } else {
-    __syncwarp();
-    __syncthreads();
-  }
-  if (warp == S::kConvWarps)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kTmem));
+  if (p.splits > 1) cluster_sync_all();          // the others have read this CTA's sums
 }
 
 template <int T, int DT>

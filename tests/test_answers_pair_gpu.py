@@ -54,3 +54,27 @@ def test_pairs_on_two_streams(gpu_lib):
     torch.cuda.synchronize()
     for (_, want, _), ys in zip(made, out):
         assert all(torch.equal(y, want) for y in ys)
+
+
+def test_all_kernels_at_once(gpu_lib):
+    """The three kernels on three streams, on each other's SMs: few samples, some dozens with the columns over clusters,
+    many."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(7)
+    made = [layer(gpu_lib, 2048, 64, 8192, 5)]
+    for rows, n_in, n_out in ((4, 4096, 16384), (48, 16000, 700), (64, 4096, 2048), (120, 8192, 1000)):
+        x = torch.randint(-127, 128, (rows, n_in), generator=g, device="cuda").to(torch.int8)
+        w = torch.randint(-127, 128, (n_out, n_in), generator=g, device="cuda").to(torch.int8)
+        one = torch.ones(max(rows, n_out), device="cuda")
+        arg = (x, one[:rows], w, one[:n_out])
+        assert gpu_lib.mca_code_linear_workspace_size(*arg) == 0
+        made.append((arg, (x.double() @ w.double().T).float(), None))
+    streams = [torch.cuda.Stream() for _ in made]
+    out = [[torch.full_like(want, float("nan")) for _ in range(12)] for _, want, _ in made]
+    torch.cuda.synchronize()
+    for i in range(12):
+        for (arg, _, ws), ys, st in zip(made, out, streams):
+            gpu_lib.mca_code_linear(*arg, out=ys[i], workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    for (_, want, _), ys in zip(made, out):
+        assert all(torch.equal(y, want) for y in ys)
