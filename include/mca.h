@@ -503,10 +503,11 @@ mca_status mca_score(mca_handle* h, float* logits, int32_t top, float* logprob, 
 /* Answers of an MLP handle's net, with its present weights, to n new samples in 8-bit integers: every layer
  * quantises its inputs per sample (mca_quantize_rows) and multiplies them with weights in 8 bits per
  * output neuron (mca_code_linear; a ternary layer's codes with its scale, other layers' effective weights
- * quantised by row). x: [n x n_in of the first layer] fp32, row stride ldx; out: [n x n_out of the last layer] fp32,
- * its activations, contiguous. Hidden activations are held in fp16 (transfer functions bounded by 1) or fp32. workspace:
- * mca_predict_workspace_size() bytes, 256-byte aligned. DEVICE arrays of the handle's device. Queued
- * on the handle's stream, without waiting. Errors: INVALID, UNSUPPORTED (a Transformer handle, or a layer beyond
+ * quantised by row). x: [n x n_in of the first layer] fp32, row stride ldx; out: [n x n_out of the last
+ * layer] fp32, its activations, contiguous. Hidden activations are held in fp16 (transfer functions bounded
+ * by 1) or fp32. workspace: mca_predict_workspace_size() bytes, 256-byte aligned. DEVICE arrays of the
+ * handle's device. Queued on the handle's stream, without waiting. Errors: INVALID, UNSUPPORTED (a
+ * Transformer handle, or a layer beyond
  * mca_code_linear's sizes), OOM (workspace too small), CUDA. */
 mca_status mca_predict_workspace_size(mca_handle* h, int64_t n, size_t* bytes);
 mca_status mca_predict(mca_handle* h, const float* x, int64_t n, int64_t ldx, float* out,

@@ -29,7 +29,6 @@ struct LogprobArgs {
 cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t s);
 cudaError_t launch_logprobs_backward(const mca_token_logprobs_backward_args& a, cudaStream_t s);
 
-// Logits of a handle's own samples from its cached fields (mca_answers.cu).
-constexpr int kMaxTop = 32;
+constexpr int kMaxTop = 32;                  // alternatives of a row
 
 }  // namespace mca

@@ -19,9 +19,12 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 //    256   4096  4096   57 / 23 / 33    512    4096  4096  - / 38 / 34
 //    512  16384  1024  100 / 40 / 86    128     784  4096  14 / 13 / 12
 // Few samples stream the weights, as long as a CTA's 32 outputs by 64 samples all run at once and their columns
-// are not too many; beyond, the cluster kernel takes about 3 us and, for each round of its CTAs, 4 us and 1.03 us for
-// every stage of 128 columns, the pair kernel 9 us, the operands' way to fp16 and back (3 bytes a code) and 4.1 ns for each column of its
-// rounds of tiles.
+// are not too many; other products of up to 64 samples take the cluster kernel. Beyond, the cluster kernel (in tiles
+// of 128 samples) takes about 3 us and, for each round of its CTAs, 4 us and 1.03 us for every stage of 128 columns,
+// the pair kernel 9 us, the operands' way to fp16 and back (3 bytes a code) and 4.1 ns for each column of its rounds
+// of tiles. Not in the rule: the copy of operands whose rows lie off 16-byte boundaries (a launch, in either of the
+// first two kernels), and few outputs, which leave most of a tile of 128 or 256 idle in both (60000 x 4096 -> 10
+// takes 167 us, 37 of them the samples' way from memory).
 Kernel choose(const mca_code_linear_args& a) {
   const int64_t rows = a.rows, n_in = a.n_in, n_out = a.n_out, sms = 152;
   if (rows <= 8) return Kernel::kStream;

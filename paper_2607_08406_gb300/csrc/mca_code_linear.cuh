@@ -28,12 +28,12 @@ __device__ __forceinline__ float act_accurate(int act, float z, float g) {
   }
 }
 
-// z Phi(z) = max(z, 0) - a Q(a), a = |z|, with the normal distribution's tail Q(a) = exp(-a^2/2) t P(t), t = 1 / (1 + p a), in
-// the form that Hastings gave (Approximations for Digital Computers, 1955); P fitted here to the tail in 64 bits, off by
-// 0.9 * 2^-24 at most. In half steps of fp32 relative to the value an output is off by at most 18 + 1.5 z^2: exponent 1.5
-// z^2 and 4 for ex2, 3 roundings of t that count 2.3 times, 3 for P's sum, 1 for its fit, 3 for the products. Tails below
-// 2^-126 are 0; the limit -0 of -infinity is taken. Pairs of fields: 13 instructions each, 241 us for 14346 x 64 -> 15616
-// fp16, where erfcf's 60 took 474.
+// z Phi(z) = max(z, 0) - a Q(a), a = |z|, with the normal distribution's tail Q(a) = exp(-a^2/2) t P(t), t = 1 / (1 +
+// p a), in the form that Hastings gave (Approximations for Digital Computers, 1955); P fitted here to the tail in 64
+// bits, off by 0.9 * 2^-24 at most. In half steps of fp32 relative to the value an output is off by at most 18 + 1.5
+// z^2: exponent 1.5 z^2 and 4 for ex2, 3 roundings of t that count 2.3 times, 3 for P's sum, 1 for its fit, 3 for the
+// products. Tails below 2^-126 are 0; the limit -0 of -infinity is taken. Pairs of fields: 13 instructions each, 245
+// us for 14346 x 64 -> 15616 fp16, where erfcf's 60 took 474.
 template <int N>
 __device__ __forceinline__ void gelu_block(float (&v)[N]) {
   static_assert(N % 2 == 0, "pairs");
@@ -177,7 +177,7 @@ inline bool code_rows_aligned(const int8_t* p, int64_t rows, int64_t ld) {
 
 // mca_code_linear_stream.cu: few samples; operands' rows on 16-byte boundaries.
 cudaError_t launch_code_linear_stream(const mca_code_linear_args& a, cudaStream_t s);
-// mca_code_linear_tc.cu: some dozens of samples; operands' rows on 16-byte boundaries. Its time by sizes.
+// mca_code_linear_tc.cu: some dozens of samples; operands' rows on 16-byte boundaries. Its time for more than 64.
 double code_linear_split_us(const mca_code_linear_args& a);
 cudaError_t launch_code_linear_split(const mca_code_linear_args& a, cudaStream_t s);
 // mca_code_linear_pair.cu: many samples; in a.workspace the operands as fp16.

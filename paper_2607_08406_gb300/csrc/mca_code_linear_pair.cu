@@ -12,16 +12,16 @@
 // memory (2 x 256 columns): while one is read, scaled and written, the next tile's MMAs run.
 //
 // The first CTA's MMAs read what both CTAs' copies brought: the copies of both (cta_group::2) count their bytes on the
-// first CTA's barrier, which orders them for the cluster. That the second CTA's sums have been read is passed on by one of
-// its threads, with the cluster's scope: an arrival of that scope takes 1200 cycles, which nothing waits for there (from
-// each warp that takes sums 14346 x 64 -> 15616 fp16 took 171 us, so
-// 157; with a thread that handed over each chunk 8192 x 8192 -> 8192 took 1600 us, so 600).
+// first CTA's barrier, which orders them for the cluster. That the second CTA's sums have been read is passed on by one
+// of its threads, with the cluster's scope: an arrival of that scope takes 1200 cycles, which nothing waits for there
+// (from each warp that takes sums 14346 x 64 -> 15616 fp16 took 171 us, so 157 on the same GPU; with a thread that
+// handed over each chunk 8192 x 8192 -> 8192 took 1600 us, so 600).
 //
-// 8192 x 8192 -> 8192: 600 us, 1.83 PFLOP/s with the conversion, the tensor cores 86 % busy. With few columns the operands'
-// way from L2 bounds it: 784 -> 4096 on 60000 samples takes 255 us (outputs fp16), 206 of them MMAs at the measured
-// peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian: 313 us). With
-// fewer still it is the outputs' instructions, 11 a field and the function's: 14346 x 64 -> 15616 fp16 takes 157 us (66 are
-// the outputs' way to memory).
+// 8192 x 8192 -> 8192: 594 us, 1.85 PFLOP/s with the conversion, the tensor cores 87 % busy. With few columns the
+// operands' way from L2 bounds it: 784 -> 4096 on 60000 samples takes 255 us (outputs fp16), 206 of them MMAs at the
+// measured peak, while 13 TB/s leave L2 and 0.5 GB of outputs are written; transfer functions add to that (Gaussian:
+// 293 us). With fewer still it is the outputs' instructions, 11 a field and the function's: 14346 x 64 -> 15616 fp16
+// takes 147 us, Gaussian 214, GELU 245 (66 are the outputs' way to memory).
 //
 // Warps: 0 copies, 1 issues MMAs (in the pair's first CTA) or passes on that sums are read (in the second), 4-19 take
 // the sums (each 32 outputs and a quarter of the samples). Sums of more than 1024 columns are added up as integers in
@@ -224,9 +224,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           copy_chunk(to + kChunk, &p.images, x + c, bar);
         }
       }
-      // The arrivals of the MMAs that read the last copies come before the CTA leaves: they are issued by the first CTA,
-      // whose own have come when the second's may still be on their way. (A wait that ran out has given the copies in
-      // flight its 2 s.)
+      // The arrivals of the MMAs that read the last copies come before the CTA leaves: they are issued by the first
+      // CTA, whose own have come when the second's may still be on their way. (A wait that ran out has given the
+      // copies in flight its 2 s.)
       for (int q = max(0, at - kStages); q < at && ok; ++q)
         ok = wait_pair(&s_free[q % kStages], (uint32_t)(q / kStages) & 1u);
     }
@@ -378,7 +378,8 @@ size_t image_bytes(int64_t rows, int n_in) {
   return (size_t)tiles_of(rows) * 2 * (size_t)((n_in + kSubK - 1) / kSubK) * kChunk;
 }
 
-// The images' n chunks as the tensor copies see them; the driver's function by its name, which needs no library to link.
+// The images' n chunks as the tensor copies see them; the driver's function by its name, which needs no library to
+// link.
 cudaError_t images_map(CUtensorMap* map, void* img, size_t n) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

@@ -7,10 +7,11 @@
 // slice has at most 1024 columns, so that its sums are exact in fp32, and adds them as integers in shared
 // memory (in any order: integers).
 //
-// What bounds it is the weights' way from memory, n_in * n_out bytes: 4096 -> 16384 takes 14 us for up to 8 samples
-// (4.9 TB/s), 22 for 16, 24 for 32, where the MMAs count, which take a warp scheduler 30 cycles each. (The tcgen05 form of this, with weights by TMA into a ring, converted by warps into tensor memory, spent most
-// of its time in hand-overs: a wait for an mbarrier takes 200 cycles even if nothing is left to wait for, and
-// a warp's share of a stage was worth 600.)
+// What bounds it are the loads in flight: 4096 -> 16384 takes 14 us for up to 8 samples, 4.9 of the 6.8 TB/s that a
+// copy reaches, with a fifth of the warps active, and 56 of its 512 CTAs run in a second wave; 22 us for 16 and 24
+// for 32, where the MMAs count, which take a warp scheduler 30 cycles each. (The tcgen05 form of this, with weights
+// by TMA into a ring, converted by warps into tensor memory, spent most of its time in hand-overs: a wait for an
+// mbarrier takes 200 cycles even if nothing is left to wait for, and a warp's share of a stage was worth 600.)
 #include <algorithm>
 
 #include "mca_code_linear.cuh"

@@ -12,8 +12,8 @@
 // units' distance is a multiple of 128 bytes plus 16, so that a quarter (two rows by four units) meets every bank once.
 //
 // 8192 -> 8192 takes 39 us for 128 samples, 32 for 64: about 1 us for a CTA's stage of 16 KB of weights, which the
-// conversions (130 instructions for 16 rows of 128 columns), the hand-overs and the loads' latency share; an M = 128 MMA
-// takes 80 cycles even for 16 samples, so that the tensor cores would allow 25 bytes of weights per cycle and SM.
+// conversions (130 instructions for 16 rows of 128 columns), the hand-overs and the loads' latency share; an M = 128
+// MMA takes 80 cycles even for 16 samples, so that the tensor cores would allow 25 bytes of weights per cycle and SM.
 //
 // Each CTA of a cluster takes a part of the columns; the sums meet as integers in shared memory, where every CTA of
 // the cluster adds up and writes its share of the samples (their order cannot change a result).
@@ -217,8 +217,8 @@ __global__ void __launch_bounds__(Shape<T>::kThreads, T > 64 ? 1 : 2) code_linea
   tc_fence_before();
   __syncwarp();
   __syncthreads();
-  // The sums are in shared memory. Tensor memory goes back before the CTA waits for others: a kernel that wants it on this
-  // SM may hold up one that the cluster's other CTAs wait for.
+  // The sums are in shared memory. Tensor memory goes back before the CTA waits for others: a kernel that wants it on
+  // this SM may hold up one that the cluster's other CTAs wait for.
   if (warp == S::kConvWarps) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kTmem));

@@ -4,14 +4,15 @@
 // + ln s and the entropy ln s - u / s. When a larger m comes along, with c the change of m, s becomes f s and u becomes
 // f (u + s c), f = exp(c). (m may lag behind by up to kLead, which see.) Differences are taken before anything
 // is scaled, so that a common shift of a row loses nothing. Both kernels read every logit once; the gradient is a
-// product per logit. The least they take is the memory's time, 30 us for 2048 x 50001 bf16 (0.2 GB at 6.8 TB/s). Measured
-// there: 45 us without alternatives, 53 with 8, and the gradient 67 of 60: some 100 instructions for 8 logits (160 of the
-// gradient) keep the schedulers 60 to 80 % busy, and rows end unevenly.
+// product per logit. The least they take is the memory's time, 30 us for 2048 x 50001 bf16 (0.2 GB at 6.8 TB/s).
+// Measured there: 45 us without alternatives, 53 with 8, and the gradient 67 of 60: some 115 instructions for 8 logits
+// (160 of the gradient) keep the schedulers 65 to 80 % busy, and rows end unevenly.
 //
 // Alternatives without a second pass: a thread keeps the largest logit of each of up to 8 groups of its 16-byte pieces.
-// The k-th largest of a row's groups is a bound that the k-th alternative cannot be below; few more than k groups reach it
-// (no more, with one warp and no equal logits), and only these are read again (from L2). What is found there is few enough
-// to be put in order by counting. (Sorting the threads' largest and merging lists over the CTA took 9 us of a row's 25.)
+// The k-th largest of a row's groups is a bound that the k-th alternative cannot be below; few more than k groups reach
+// it (no more, with one warp and no equal logits), and only these are read again (from L2). What is found there is few
+// enough to be put in order by counting. (Sorting the threads' largest and merging lists over the CTA took 9 us of a
+// row's 25.)
 #include <algorithm>
 
 #include "mca_answers.h"
@@ -99,7 +100,7 @@ __device__ __forceinline__ void write_top(const mca_token_logprobs_args& a, int6
 constexpr int kSmallThreads = 128;
 constexpr int kSmallVocab = 1024;
 // Up to which the rounds of the small kernel find several alternatives faster, and rows below which its latency counts:
-// 20000 x 1000 bf16 with 8 takes 74 us in rounds and 34 otherwise, 20000 x 200 with 5 20 and 25, 100 x 500 4 and 6.
+// 20000 x 1000 bf16 with 8 takes 74 us in rounds and 38 otherwise, 20000 x 200 with 5 17 and 25, 100 x 500 4 and 6.
 constexpr int kRoundVocab = 256;
 constexpr int kRoundRows = 2048;
 
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(kSmallThreads) logprobs_small_kernel(LogprobAr
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kAhead = 4;                 // pieces that a thread has on their way (51 us; 6: 53, 8: 54)
+constexpr int kAhead = 4;                 // pieces that a thread has on their way (took 51 us; 6: 53, 8: 54)
 constexpr int kGroups = 8;                // groups of a thread's pieces
 constexpr int kTeamVocab = 2048;          // a warp per row up to this vocabulary
 
@@ -183,7 +184,9 @@ struct Pieces {
     count = (int)(((int64_t)V + head + N - 1) / N);
   }
   __device__ __forceinline__ int index(int j, int i) const { return j * N - head + i; }
-  __device__ __forceinline__ bool whole(int j) const { return j * N >= head && (int64_t)(j + 1) * N <= (int64_t)V + head; }
+  __device__ __forceinline__ bool whole(int j) const {
+    return j * N >= head && (int64_t)(j + 1) * N <= (int64_t)V + head;
+  }
   __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(x - head); }
   __device__ __forceinline__ uint4 raw(int j) const { return pieces()[j]; }
   __device__ __forceinline__ static void values(const uint4& q, float (&v)[N]) {
@@ -284,11 +287,11 @@ __device__ __forceinline__ float clamp_piece(const uint4& q, float2 (&v)[Pieces<
 }
 
 // What a thread has seen. The sums refer to m, which follows the largest logit only when that is more than kLead above
-// it: most pieces take no rescaling, and a row that rises slowly takes one for each kLead, not for each piece (every one is
-// off by some half steps, 2^-24: by steps of 0.01, the entropy by 76 without a lead and 4 with one). The price is
-// that u holds terms of either sign, up to kLead e^kLead, before the last shift, which takes their roundings along: with
-// 1 those are some half steps of s more, with 8 the entropy of 80011 logits of which all but some were equal was off by
-// 1900. 2048 x 50001 bf16 without alternatives takes 45.0, 44.4 and 43.5 us with 0, 1 and 8.
+// it: most pieces take no rescaling, and a row that rises slowly takes one for each kLead, not for each piece (every
+// one is off by some half steps, 2^-24: by steps of 0.01, the entropy by 76 without a lead and 4 with one). The price
+// is that u holds terms of either sign, up to kLead e^kLead, before the last shift, which takes their roundings
+// along: with 1 those are some half steps of s more, with 8 the entropy of 80011 logits of which all but some were
+// equal was off by 1900. 2048 x 50001 bf16 without alternatives takes 45.0, 44.4 and 43.5 us with 0, 1 and 8.
 constexpr float kLead = 1.0f;
 
 //
@@ -379,8 +382,9 @@ __device__ __forceinline__ Sums team_sums(Sums t, Team<W>& s) {
   return t;
 }
 
-// The candidates: the logits that reach the bound, which lie in the groups whose largest does. Their pieces are read again
-// by the whole CTA, all at once. A thread's group g holds its pieces g size .. of the order that it took them in.
+// The candidates: the logits that reach the bound, which lie in the groups whose largest does. Their pieces are read
+// again by the whole CTA, all at once. A thread's group g holds its pieces g size .. of the order that it took them
+// in.
 template <int DT, int W>
 __device__ __forceinline__ void find_candidates(const Pieces<DT>& row, int j0, int j1, int size, float top, Key bound,
                                                 Team<W>& s) {
@@ -421,8 +425,8 @@ __device__ __forceinline__ Key exchange(Key k, int j, bool larger) {
   return (q > k) == larger ? q : k;
 }
 
-// Lists of the n <= 32 largest keys, a key per lane in falling order: q of every lane into it. What lies behind the n-th is
-// one of the keys, and not looked at.
+// Lists of the n <= 32 largest keys, a key per lane in falling order: q of every lane into it. What lies behind the
+// n-th is one of the keys, and not looked at.
 __device__ __forceinline__ void keep_largest(Key& mine, Key q, int n) {
   const int lane = threadIdx.x & 31;
   unsigned int found = __ballot_sync(0xffffffffu, q > __shfl_sync(0xffffffffu, mine, n - 1));
@@ -490,9 +494,9 @@ __device__ __noinline__ void ordered_top(const elem_t<DT>* x, int V, int j0, int
   merge_lists<W>(mine, s);
 }
 
-// The largest n of a row's logits up to `limit`, in order, and how many they are at s.cand and s.n. A warp's pieces lie in
-// the order of their index: of equal logits, as a mask leaves them, the first are kept and the others end at the vote.
-// (2048 x 50001 bf16, 5 symbols left of 8 asked for: 104 us, where a pass for each alternative took 600.)
+// The largest n of a row's logits up to `limit`, in order, and how many they are at s.cand and s.n. A warp's pieces
+// lie in the order of their index: of equal logits, as a mask leaves them, the first are kept and the others end at
+// the vote. (2048 x 50001 bf16, 5 symbols left of 8 asked for: 104 us, where a pass for each alternative took 600.)
 template <int DT, int W>
 __device__ __noinline__ void rest_of_top(const elem_t<DT>* x, int V, float limit, int n, Team<W>& s) {
   const Pieces<DT> row(x, V);
@@ -524,7 +528,8 @@ __device__ __noinline__ void rest_of_top(const elem_t<DT>* x, int V, float limit
   merge_lists<W>(mine, s);
 }
 
-// Any row, by the definition: passes for the largest logit, and, unless that says it all, for the sums and the alternatives.
+// Any row, by the definition: passes for the largest logit, and, unless that says it all, for the sums and the
+// alternatives.
 template <int DT, int W>
 __device__ __noinline__ void exact_row(const LogprobArgs& p, int64_t r, Team<W>& s) {
   const mca_token_logprobs_args& a = p.a;
@@ -607,8 +612,8 @@ __global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p,
   Seen<DT> seen;
   const int size = ((j1 - j0 + kTeam - 1) / kTeam + kGroups - 1) / kGroups;     // of a group
   {
-    // kAhead pieces on their way to shared memory, each to its thread's own places: no registers, no barriers. A piece at an
-    // end of the row that is not whole is put there by its thread.
+    // kAhead pieces on their way to shared memory, each to its thread's own places: no registers, no barriers. A
+    // piece at an end of the row that is not whole is put there by its thread.
     const unsigned int ring = (unsigned int)__cvta_generic_to_shared(&s_ring[0][tid]);
     constexpr unsigned int kSlot = kTeam * 16;
     const int w0 = row.whole(0) ? 0 : 1, whole = row.count - w0 - (row.whole(row.count - 1) ? 0 : 1);
@@ -660,9 +665,9 @@ __global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p,
 
   // the candidates: logits that reach the bound
   if (a.top > 0) {
-    // a warp's k / W-th largest group, of equal ones all at once; k groups reach the smallest of the warps' (one thread's
-    // largest in place of each group's let through 130 logits for 32 alternatives and one warp, and half the row: 4096 x
-    // 32000 bf16 315 us, so 87; with 20 alternatives 86 and 76)
+    // a warp's k / W-th largest group, of equal ones all at once; k groups reach the smallest of the warps' (one
+    // thread's largest in place of each group's let through 130 logits for 32 alternatives and one warp, and half the
+    // row: 4096 x 32000 bf16 315 us, so 87; with 20 alternatives 86 and 76)
     unsigned int v[kGroups], reach = 0u;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
@@ -722,7 +727,8 @@ __global__ void __launch_bounds__(32 * W, 32 / W) logprobs_kernel(LogprobArgs p,
   int found = n;
   if (kWhole && split > 1 && a.top > 0) {                        // empty places of the lists
     found = 0;
-    for (int q = 0; q < n; q += 32) found += __popc(__ballot_sync(0xffffffffu, q + lane < n && s_best[q + lane] != 0ull));
+    for (int q = 0; q < n; q += 32)
+      found += __popc(__ballot_sync(0xffffffffu, q + lane < n && s_best[q + lane] != 0ull));
   }
   if (t.m <= Range<DT>::high) {
     __syncwarp();
@@ -796,7 +802,8 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_small_kernel(mca_t
 }
 
 // kGradAhead pieces per thread of a row; logits and gradient lie at the same distance from 16-byte boundaries. (2048 x
-// 50001 bf16: 66 us with two, 71 with four; the 32 bytes of one thread side by side took 83 when two took 69.)
+// 50001 bf16: 66 us with two, 71 with four; the 32 bytes of one thread side by side took 83 when two took 69. Matrices
+// that lie differently there go element by element: 208 us for bf16 logits padded to 50008 and a contiguous gradient.)
 constexpr int kGradAhead = 2;
 
 template <int DT>
@@ -878,7 +885,7 @@ cudaError_t launch_logprobs_t(const LogprobArgs& p, cudaStream_t s) {
     return cudaGetLastError();
   }
   // Warps per row: as many as run at once, so that all rows do; one for short rows (a CTA's threads would have no piece
-  // each). 2048 x 50001 bf16 with 8 alternatives takes 51 us with two, 64 with eight in more than two waves.
+  // each). 2048 x 50001 bf16 with 8 alternatives took 51 us with two, 64 with eight in more than two waves.
   const int64_t warps = 32 * 152 / p.a.rows;
   if (V <= kTeamVocab || warps < 2) return launch_team<DT, 1>(p, s);
   if (warps < 4) return launch_team<DT, 2>(p, s);

@@ -632,7 +632,9 @@ def _addr(t):
 
 def mca_token_logprobs(logits, targets=None, top: int = 0, stream=None) -> TokenLogprobs:
     """Log probabilities of targets [rows] (int32, -1: none) under softmax of each row of logits [rows,
-    vocab], entropies, log-sum-exps and the `top` most probable symbols (at most 32)."""
+    vocab], entropies, log-sum-exps and the `top` most probable symbols (at most 32). No operation of
+    torch's autograd: of logits that require a gradient the results carry none;
+    mca_token_logprobs_backward computes it."""
     _ready()
     rows, vocab, ld = _matrix("logits", logits, _dtypes)
     dev = logits.get_device()
