@@ -78,3 +78,25 @@ def test_all_kernels_at_once(gpu_lib):
     torch.cuda.synchronize()
     for (_, want, _), ys in zip(made, out):
         assert all(torch.equal(y, want) for y in ys)
+
+
+def test_two_graphs_of_pairs(gpu_lib):
+    """Two captured layers replayed at the same time: each has the images of its own operands."""
+    import torch
+    made = []
+    for seed, rows, n_in, n_out in ((8, 2048, 64, 8192), (9, 1200, 2000, 3001)):
+        arg, want, _ = layer(gpu_lib, rows, n_in, n_out, seed)
+        gpu_lib.mca_code_linear(*arg)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = gpu_lib.mca_code_linear(*arg)
+        made.append((graph, y, want, torch.cuda.Stream(), arg))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for graph, y, _, st, _ in made:
+            with torch.cuda.stream(st):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, y, want, *_ in made:
+        assert torch.equal(y, want)

@@ -96,3 +96,35 @@ def test_inputs_freed_while_their_work_waits(gpu_lib, which, raw):
     assert not {a.data_ptr() for a in again} & {p for _, _, p in sizes}, name
     torch.cuda.synchronize()
     assert all(torch.equal(u, v) for u, v in zip(got, want)), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [33, 2048])
+def test_captured_on_another_stream(gpu_lib, rows):
+    """The chain on a stream that a capture has taken in, replayed on new inputs: bit for bit the eager results."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    n_in, vocab = 256, 3001
+    xs = [torch.randn(rows, n_in, generator=g, device="cuda") for _ in range(2)]
+    w = torch.randint(-127, 128, (vocab, n_in), generator=g, device="cuda").to(torch.int8)
+    ws = torch.rand(vocab, generator=g, device="cuda") * 1e-3
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+
+    def chain(x, stream):
+        q, s = gpu_lib.mca_quantize_rows(x, stream=stream)
+        y = gpu_lib.mca_code_linear(q, s, w, ws, dtype=torch.float16, stream=stream)
+        r = gpu_lib.mca_token_logprobs(y, t, top=4, stream=stream)
+        return [q, s, y, *r, gpu_lib.mca_token_logprobs_backward(y, t, r.lse, r.entropy, r.logprob, r.entropy,
+                                                                 stream=stream)]
+    want = [chain(x, None) for x in xs]
+    buf, side, graph = xs[0].clone(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = chain(buf, side)
+        torch.cuda.current_stream().wait_stream(side)
+    for x, ref in ((xs[1], want[1]), (xs[0], want[0])):
+        buf.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
