@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kSmallThreads) distill_small_kernel(mca_distil
   uint4 q[P];
 #pragma unroll
   for (int i = 0; i < P; ++i)
-    if (lane + 32 * i < row.count) q[i] = block_of(row, lane + 32 * i);
+    if (lane + 32 * i < row.count) q[i] = row.bits(lane + 32 * i);
   t.resolve(a);
   float x[kPerLane];
   List::each(a.top, [&](int k) { x[k] = t.symbol[k] >= 0 ? elem_f32(row.x[t.symbol[k]]) : 0.0f; });
@@ -669,7 +669,8 @@ constexpr int kRowPieces = 3200;          // of a row at most
 
 template <int DT, int W>
 __global__ void __launch_bounds__(32 * W) distill_row_kernel(mca_distill_args a, float c) {
-  constexpr int N = Pieces<DT>::N, kTeam = 32 * W;
+  using P = Pieces<DT>;
+  constexpr int N = P::N, kTeam = 32 * W;
   extern __shared__ uint4 s_row[];
   __shared__ float s_part[2][W];
   const int64_t r = blockIdx.x;
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(32 * W) distill_row_kernel(mca_distill_args a,
     if (row.whole(j))
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(row.pieces() + j) : "memory");
     else
-      s_row[j] = block_of(row, j);
+      s_row[j] = P::part(row.x, row.V, row.index(j, 0));
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
   List t;
@@ -1049,7 +1050,8 @@ __device__ __forceinline__ uint4 pack(const float2 (&v)[Pieces<DT>::N / 2]) {
 }
 
 // The rows of logits and gradient, by 16-byte pieces of the gradient. SAME: both lie at the same distance from 16-byte
-// boundaries; otherwise a piece's logits are cut from the two 16-byte blocks that hold them.
+// boundaries; otherwise a piece's logits are cut from the two 16-byte blocks that hold them, or read one by one where
+// these hold more than the row's own.
 template <int DT, bool SAME>
 struct GradRow {
   using P = Pieces<DT>;
@@ -1058,8 +1060,8 @@ struct GradRow {
   elem_t<DT>* out;
   P row;                                  // of the gradient
   const uint4* blocks;
-  unsigned int by, whole;
-  int first;                              // whole pieces from here on
+  unsigned int by, whole, own;
+  int first, own_first;                   // whole pieces, and those that are cut from the row's own blocks, from here on
 
   __device__ __forceinline__ GradRow(const mca_distill_backward_args& a, int64_t r)
       : x(static_cast<const elem_t<DT>*>(a.logits) + r * a.ld), out(static_cast<elem_t<DT>*>(a.grad) + r * a.ldg),
@@ -1069,14 +1071,18 @@ struct GradRow {
     blocks = reinterpret_cast<const uint4*>(from - by);
     first = row.whole(0) ? 0 : 1;
     whole = (unsigned int)max(0, row.count - (row.whole(row.count - 1) ? 0 : 1) - first);
+    own_first = SAME ? first : first_of_own_blocks(row.head, (int)by, (int)sizeof(elem_t<DT>));
+    own = SAME ? whole
+               : (unsigned int)max(0, end_of_own_blocks(row.V, row.head, (int)by, (int)sizeof(elem_t<DT>)) - own_first);
   }
   __device__ __forceinline__ bool is_whole(int j) const { return (unsigned int)(j - first) < whole; }
-  // The logits of piece j: of a whole one as they are, cut() from two blocks where they lie differently.
+  __device__ __forceinline__ bool is_own(int j) const { return (unsigned int)(j - own_first) < own; }
+  // The logits of piece j as they are, or the two blocks that they are cut from.
   struct Raw {
     uint4 lo, hi;
   };
   __device__ __forceinline__ void ask(int j, Raw& q) const {
-    if (is_whole(j)) {
+    if (is_own(j)) {
       q.lo = blocks[j];
       if (!SAME && by) q.hi = blocks[j + 1];           // (behind a row that lies alike may be nothing)
     } else {
@@ -1087,7 +1093,7 @@ struct GradRow {
     const bool all = is_whole(j);
     float v[N];
     float2 d[N / 2];
-    P::values(SAME || !all ? raw.lo : shifted(raw.lo, raw.hi, by), v);
+    P::values(SAME || !is_own(j) ? raw.lo : shifted(raw.lo, raw.hi, by), v);
 #pragma unroll
     for (int e = 0; e < N; e += 2) d[e / 2] = w.others<DT>(make_float2(v[e], v[e + 1]));
     const uint4 o = pack<DT>(d);

@@ -329,14 +329,20 @@ __device__ __forceinline__ int log2_of(int power) { return 31 - __clz(power); }
 
 // A warp's part of a row: pieces from .. to, lane by lane; its sums after each of kGroups groups of rounds stay in `kept`.
 struct Span {
-  int from, to, rounds, group, first, whole;           // of which `whole` pieces from `first` on are
+  int from, to, rounds, group, first, whole;           // of which `whole` pieces from `first` on are, of both rows
   // Part `part` of 2^shift.
-  template <int DT>
-  __device__ __forceinline__ Span(const Pieces<DT>& row, int part, int shift)
-      : from((int)((int64_t)row.count * part >> shift)), to((int)((int64_t)row.count * (part + 1) >> shift)),
+  template <int DT, bool RES>
+  __device__ __forceinline__ Span(const Source<DT, RES>& src, int part, int shift)
+      : from((int)((int64_t)src.row.count * part >> shift)), to((int)((int64_t)src.row.count * (part + 1) >> shift)),
         rounds((to - from + 31) / 32), group(max(1, (rounds + kGroups - 1) / kGroups)) {
-    first = max(from, row.whole(0) ? 0 : 1);
-    whole = max(0, min(to, row.count - (row.whole(row.count - 1) ? 0 : 1)) - first);
+    const Pieces<DT>& row = src.row;
+    int lo = row.whole(0) ? 0 : 1, hi = row.count - (row.whole(row.count - 1) ? 0 : 1);
+    if (RES) {
+      lo = max(lo, first_of_own_blocks(row.head, (int)src.by, (int)sizeof(elem_t<DT>)));
+      hi = min(hi, end_of_own_blocks(row.V, row.head, (int)src.by, (int)sizeof(elem_t<DT>)));
+    }
+    first = max(from, lo);
+    whole = max(0, min(to, hi) - first);
   }
   __device__ __forceinline__ bool is_whole(int j) const { return (unsigned int)(j - first) < (unsigned int)whole; }
 };
@@ -631,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(mca_sample_toke
   // (rows behind the last one: none is read)
   Source<DT, false> src(static_cast<const elem_t<DT>*>(a.logits) + min(r, a.rows - 1) * a.ld, nullptr, a.vocab);
   const P& row = src.row;
-  const Span span(row, rank * W + warp % W, log2_of(W * split));
+  const Span span(src, rank * W + warp % W, log2_of(W * split));
   typename Source<DT, false>::Raw only;
   if (ROUND)
     only = src.ask(lane, r < a.rows && span.is_whole(lane));
@@ -805,7 +811,7 @@ __device__ __forceinline__ void draw_last(const mca_verify_drafts_args& a, int64
     src.ry = d.ry;
     src.fx = floor_word<DT>(lx - kFloor);
     src.fy = floor_word<DT>(ly - kFloor);
-    const Span span(src.row, rank * W + warp % W, log2_of(W * split));
+    const Span span(src, rank * W + warp % W, log2_of(W * split));
     float mx = -INFINITY, my = -INFINITY;
     auto look = [&](const auto& p, int) {
       mx = max_nan(mx, largest<DT>(p.x));

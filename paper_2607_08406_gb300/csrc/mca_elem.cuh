@@ -30,7 +30,7 @@ __device__ __forceinline__ float elem_f32(__half v) { return __half2float(v); }
 __device__ __forceinline__ float elem_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 template <int DT>
-__device__ __forceinline__ elem_t<DT> elem_of(float v) {
+__host__ __device__ __forceinline__ elem_t<DT> elem_of(float v) {
   if constexpr (DT == MCA_DTYPE_FP32)
     return v;
   else if constexpr (DT == MCA_DTYPE_FP16)

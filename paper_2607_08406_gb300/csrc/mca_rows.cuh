@@ -30,16 +30,16 @@ struct Pieces {
   static constexpr int N = 16 / (int)sizeof(elem_t<DT>);
   const elem_t<DT>* x;
   int V, head, count;
-  __device__ __forceinline__ Pieces(const elem_t<DT>* x_, int V_) : x(x_), V(V_) {
+  __host__ __device__ __forceinline__ Pieces(const elem_t<DT>* x_, int V_) : x(x_), V(V_) {
     head = (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(elem_t<DT>));
     count = (int)(((int64_t)V + head + N - 1) / N);
   }
-  __device__ __forceinline__ int index(int j, int i) const { return j * N - head + i; }
-  __device__ __forceinline__ bool whole(int j) const {
+  __host__ __device__ __forceinline__ int index(int j, int i) const { return j * N - head + i; }
+  __host__ __device__ __forceinline__ bool whole(int j) const {
     return j * N >= head && (int64_t)(j + 1) * N <= (int64_t)V + head;
   }
-  __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(x - head); }
-  __device__ __forceinline__ uint4 raw(int j) const { return pieces()[j]; }
+  __host__ __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(x - head); }
+  __host__ __device__ __forceinline__ uint4 raw(int j) const { return pieces()[j]; }
   __device__ __forceinline__ static void values(const uint4& q, float (&v)[N]) {
     const unsigned int w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -53,10 +53,10 @@ struct Pieces {
     }
   }
   // Any piece of the row, -inf in the place of what is outside.
-  __device__ __forceinline__ uint4 bits(int j) const {
+  __host__ __device__ __forceinline__ uint4 bits(int j) const {
     return whole(j) ? raw(j) : part(x, V, index(j, 0));
   }
-  __device__ __noinline__ static uint4 part(const elem_t<DT>* x, int V, int at) {
+  __host__ __device__ __noinline__ static uint4 part(const elem_t<DT>* x, int V, int at) {
     union {
       elem_t<DT> e[N];
       uint4 u;
@@ -88,28 +88,13 @@ __device__ __forceinline__ float largest(const uint4& q) {
   }
 }
 
-// Piece j of a row as the 16-byte block that it is in memory, -inf in the place of what is outside the row. (A block that
-// holds some of the row is read whole: it lies within a page.)
-template <int DT>
-__device__ __forceinline__ uint4 block_of(const Pieces<DT>& row, int j) {
-  uint4 q = row.raw(j);
-  if (!row.whole(j)) {
-    constexpr unsigned int kNone = DT == MCA_DTYPE_FP32 ? 0xff800000u : DT == MCA_DTYPE_FP16 ? 0xfc00u : 0xff80u;
-    unsigned int w[4] = {q.x, q.y, q.z, q.w};
-    const int at = row.index(j, 0);
-#pragma unroll
-    for (int e = 0; e < Pieces<DT>::N; ++e) {
-      const bool in = at + e >= 0 && at + e < row.V;
-      if constexpr (DT == MCA_DTYPE_FP32)
-        w[e] = in ? w[e] : kNone;
-      else if (e & 1)
-        w[e / 2] = in ? w[e / 2] : (w[e / 2] & 0xffffu) | kNone << 16;
-      else
-        w[e / 2] = in ? w[e / 2] : (w[e / 2] & 0xffff0000u) | kNone;
-    }
-    q = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  return q;
+// Rows whose pieces are cut from two 16-byte blocks, because they lie `by` bytes behind the pieces of another row of V
+// elements (`head` of them less in its first piece): the first of the pieces whose blocks hold the row's own elements
+// alone, and the one behind the last. What else a block at an end of the row holds is not the caller's to read from.
+__host__ __device__ inline int first_of_own_blocks(int head, int by, int bytes) { return (head * bytes + by + 15) / 16; }
+__host__ __device__ inline int end_of_own_blocks(int V, int head, int by, int bytes) {
+  const int64_t to = (int64_t)(V + head) * bytes + by;         // from the first block's start to the row's end
+  return (int)(to / 16) - (by ? 1 : 0);
 }
 
 // The 16 bytes that start `by` bytes (a multiple of 2) behind the start of lo.
