@@ -402,7 +402,8 @@ __device__ __forceinline__ int symbol_at(const Source<DT, RES>& src, int j, cons
   return __shfl_sync(0xffffffffu, src.row.index(j, k < 0 ? last : k), here ? __ffs(here) - 1 : 31 - __clz(some));
 }
 
-// The symbol where a span's cumulative sum passes t, by its warp; the last one with a weight where shifts keep it below.
+// The symbol where a span's cumulative sum passes t, by its warp; the last one with a weight where shifts keep it below; -1
+// if the group that t lies in was added up in steps so much finer than the last ones that in these it has no weight.
 template <int DT, bool RES>
 __device__ __noinline__ int find_in_span(Source<DT, RES> src, Span s, const Table& table, const Kept& kept, long long t) {
   constexpr int N = Source<DT, RES>::N, kEach = 32 / kGroups;
@@ -711,6 +712,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) sample_kernel(mca_sample_toke
     if (!ROUND) {
       if (t < 0) return;
       token = find_in_span(src, span, s.table, kept, t);
+      double total;                                              // (the whole row by the warp alone)
+      if (token < 0)
+        token = exact_draw<DT, 1>({row.x, nullptr, (double)all.l * kStepAll, 0.0}, a.vocab, u, total, s.exact);
     }
     lse = ln_pair(all.total, all.l, s.table);
   }
