@@ -1322,8 +1322,8 @@ cudaError_t launch_small(const mca_distill_args& a, float c, cudaStream_t s) {
 
 template <int DT, int W>
 cudaError_t launch_row(const mca_distill_args& a, float c, int64_t count, cudaStream_t s) {
-  const size_t bytes = (size_t)count * 16;
-  if (bytes > 48 << 10) {
+  const size_t bytes = (size_t)count * 16, beside = 2 * W * sizeof(float);         // (s_part)
+  if (bytes + beside > 48 << 10) {
     const cudaError_t e = cudaFuncSetAttribute(distill_row_kernel<DT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                kRowPieces * 16);
     if (e != cudaSuccess) return e;
