@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kSmallThreads) distill_small_kernel(mca_distil
 }
 
 // ------------------------------------------------------------------------------------------------
-// Large vocabularies: W warps per row, a CTA, or the CTAs of a cluster.
+// Large vocabularies: four or eight warps per row, or the CTAs of a cluster.
 // ------------------------------------------------------------------------------------------------
 constexpr int kWarps = 8;                 // of a CTA that has a row or a part of one
 constexpr int kMaxCluster = 8;
@@ -619,18 +619,16 @@ __global__ void __launch_bounds__(32 * W, 32 / W) distill_kernel(mca_distill_arg
   Part out = sum.part(), in{-kFar, 0.0f};
   int any = TAIL && __any_sync(0xffffffffu, sum.any());
   out.join_lanes();
-  if constexpr (W > 1) {
-    if ((tid & 31) == 0) {
-      s_warp[warp] = out;
-      s_any[warp] = any;
-    }
-    team_sync<W>();
-    if (warp == 0) {
-      out = s_warp[0];
-      for (int q = 1; q < W; ++q) {
-        out.join(s_warp[q]);
-        any |= s_any[q];
-      }
+  if ((tid & 31) == 0) {
+    s_warp[warp] = out;
+    s_any[warp] = any;
+  }
+  team_sync<W>();
+  if (warp == 0) {
+    out = s_warp[0];
+    for (int q = 1; q < W; ++q) {
+      out.join(s_warp[q]);
+      any |= s_any[q];
     }
   }
   if constexpr (TAIL) {
@@ -1352,10 +1350,7 @@ cudaError_t launch_distill_t(const mca_distill_args& a, cudaStream_t s) {
     if (count <= 1024) return launch_row<DT, 2>(a, c, count, s);
     if (count <= (a.tail ? kRowPieces : 2048)) return launch_row<DT, 4>(a, c, count, s);
   }
-  // Warps per row: as many as run at once, so that all rows do, and four for long rows, however many there are (a warp of
-  // its own for each row leaves too few of them, 4096 x 128000 bf16 329 us, 205 with two, 179 with four, 189 with eight;
-  // 2048 x 50001 74, 49, 45, 50; 4096 x 32000 fp16 with tail 106, 79, 66, 92).
-  const int64_t bytes = (int64_t)V * (int64_t)sizeof(elem_t<DT>), warps = 32 * 152 / a.rows;
+  const int64_t bytes = (int64_t)V * (int64_t)sizeof(elem_t<DT>);
   // CTAs that stay where rows are long enough for one warp to keep up with their lists, and leave few of them without a
   // row at the end (4096 x 128000 179 us -> 162, 2048 x 50001 45 -> 39, 4096 x 32000 fp16 with tail 66 -> 54).
   constexpr int64_t kCtas = 152 * kStreamCtas;
@@ -1367,9 +1362,10 @@ cudaError_t launch_distill_t(const mca_distill_args& a, cudaStream_t s) {
       distill_stream_kernel<DT, false><<<(unsigned int)kCtas, kStreamThreads, 0, s>>>(a, c);
     return cudaGetLastError();
   }
-  if (warps < 2 && bytes < 16384) return launch_team<DT, 1>(a, c, 1, s);
-  if (warps < 4 && bytes < 32768) return launch_team<DT, 2>(a, c, 1, s);
-  if (warps < 8) return launch_team<DT, 4>(a, c, 1, s);
+  // Else four warps for a row, however many rows there are (4096 x 128000 bf16 329 us with one, 205 with two, 179 with
+  // four, 189 with eight; 2048 x 50001 74, 49, 45, 50; 4096 x 32000 fp16 with tail 106, 79, 66, 92; 4000 x 16380 bf16, not
+  // long enough for the above, 37 with two, 29 with four), or eight where all rows run at once with these.
+  if (a.rows * kWarps > 32 * 152) return launch_team<DT, 4>(a, c, 1, s);
   int split = 1;
   while (split < kMaxCluster && a.rows * split * 2 <= 152 && V / (split * 2) >= 2048) split *= 2;
   return launch_team<DT, kWarps>(a, c, split, s);

@@ -102,3 +102,14 @@ def test_pieces_at_the_borders(gpu_lib, dtype, border, more, last):
         x[9, vocab - 1] = float("nan")
         x[10, : vocab - 2] = float("-inf")
         check_picked(gpu_lib, x, index, t, 1.0, tail, torch.tensor([0, 1, 7, 8, 9, 10, 304, rows - 1], device="cuda"), dtype)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1300, 16380, "bfloat16"), (1300, 16383, "float16"), (1300, 8190, "float32"),
+                                              (2500, 16378, "bfloat16"), (2500, 8191, "float32")])
+def test_rows_too_long_for_shared_memory_and_too_short_to_stay(gpu_lib, rows, vocab, dtype):
+    import torch
+    x, index, t = case(vocab, rows, vocab, dtype, 24, 1, 1)
+    x[8] = float("-inf")
+    x[9, vocab - 1] = float("nan")
+    x[10, : vocab - 2] = float("-inf")
+    check_picked(gpu_lib, x, index, t, 1.0, False, torch.tensor([0, 1, 8, 9, 10, 1299, rows - 1], device="cuda"), dtype)
