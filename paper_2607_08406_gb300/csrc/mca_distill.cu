@@ -11,6 +11,7 @@
 #include "mca_answers.h"
 #include "mca_device.cuh"
 #include "mca_elem.cuh"
+#include "mca_row_shapes.h"
 #include "mca_rows.cuh"
 
 namespace mca {
@@ -258,7 +259,6 @@ __device__ __forceinline__ uint4 without(const uint4& q, unsigned int bits) {
 // (60000 x 300 bf16 against 32 symbols: 130 us with a warp and a ring of pieces for each, here 35, and 43 with tail).
 // ------------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 128;
-constexpr int kSmallPieces = 256;         // of a row at most: 8 to a lane
 
 template <int DT, int P>
 __global__ void __launch_bounds__(kSmallThreads) distill_small_kernel(mca_distill_args a, float c) {
@@ -339,8 +339,7 @@ __global__ void __launch_bounds__(kSmallThreads) distill_small_kernel(mca_distil
 // ------------------------------------------------------------------------------------------------
 // Large vocabularies: four or eight warps per row, or the CTAs of a cluster.
 // ------------------------------------------------------------------------------------------------
-constexpr int kWarps = 8;                 // of a CTA that has a row or a part of one
-constexpr int kMaxCluster = 8;
+constexpr int kWarps = kTeamWarps;
 constexpr int kAhead = 4;                 // pieces that a thread has on their way
 constexpr float kLead = 10.0f;            // how far (in units of 2) a logit may be above the reference of the sum
 
@@ -663,8 +662,6 @@ __global__ void __launch_bounds__(32 * W, 32 / W) distill_kernel(mca_distill_arg
 // takes beside its logits is not their all: twice as many take 10000 x 10000 bf16 66 us for 47, half as many 20000 x 4000
 // fp32 69 for 55. Rows of more than 2048 pieces pay with tail (6000 x 20000 bf16 66 for 72 us, 10000 x 10000 fp32 77 for
 // 101 at the time), where whole CTAs tell listed symbols apart; without they do not (61 for 46, 73 for 64).
-constexpr int kRowPieces = 3200;          // of a row at most
-
 template <int DT, int W>
 __global__ void __launch_bounds__(32 * W) distill_row_kernel(mca_distill_args a, float c) {
   using P = Pieces<DT>;
@@ -773,8 +770,6 @@ __global__ void __launch_bounds__(32 * W) distill_row_kernel(mca_distill_args a,
 // memory's rate; 2048 x 50001 39, with five rows to a CTA of 4.5; 4096 x 32000 fp16 with tail 54, instructions.
 constexpr int kStreamWarps = 8;
 constexpr int kStreamThreads = 32 * kStreamWarps + 64;
-constexpr int kStreamCtas = 3;            // per SM
-constexpr int64_t kStreamVocab = 1 << 20; // a thread adds up its terms one after the other, 1024 then
 
 struct Prepared {
   int symbol[kMaxList];
@@ -1304,13 +1299,6 @@ __global__ void __launch_bounds__(kStreamTeam + 32, kBackCtas)
 
 float scale_of(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 
-// Pieces of the longest row, wherever it starts.
-template <int DT>
-int64_t pieces_of(int64_t vocab) {
-  constexpr int N = Pieces<DT>::N;
-  return (vocab + 2 * N - 2) / N;
-}
-
 template <int DT, int P>
 cudaError_t launch_small(const mca_distill_args& a, float c, cudaStream_t s) {
   constexpr int kRows = kSmallThreads / 32;
@@ -1338,37 +1326,29 @@ cudaError_t launch_team(const mca_distill_args& a, float c, int split, cudaStrea
 
 template <int DT>
 cudaError_t launch_distill_t(const mca_distill_args& a, cudaStream_t s) {
-  const int V = a.vocab;
   const float c = scale_of(a.temperature);
-  const int64_t count = pieces_of<DT>(V);
-  if (count <= 32) return launch_small<DT, 1>(a, c, s);
-  if (count <= 64) return launch_small<DT, 2>(a, c, s);
-  if (count <= 128) return launch_small<DT, 4>(a, c, s);
-  if (count <= kSmallPieces) return launch_small<DT, 8>(a, c, s);
-  if (a.rows >= 4 * 152) {
-    if (count <= 512) return launch_row<DT, 1>(a, c, count, s);
-    if (count <= 1024) return launch_row<DT, 2>(a, c, count, s);
-    if (count <= (a.tail ? kRowPieces : 2048)) return launch_row<DT, 4>(a, c, count, s);
+  const DistillShape h = distill_shape(a.rows, a.vocab, Pieces<DT>::N, a.tail != 0);
+  switch (h.by) {
+    case DistillBy::kRegisters:
+      if (h.n == 1) return launch_small<DT, 1>(a, c, s);
+      if (h.n == 2) return launch_small<DT, 2>(a, c, s);
+      if (h.n == 4) return launch_small<DT, 4>(a, c, s);
+      return launch_small<DT, 8>(a, c, s);
+    case DistillBy::kSharedRow: {
+      const int64_t count = most_pieces(a.vocab, Pieces<DT>::N);
+      if (h.n == 1) return launch_row<DT, 1>(a, c, count, s);
+      if (h.n == 2) return launch_row<DT, 2>(a, c, count, s);
+      return launch_row<DT, 4>(a, c, count, s);
+    }
+    case DistillBy::kStaying:
+      if (a.tail)
+        distill_stream_kernel<DT, true><<<kSms * kStreamCtas, kStreamThreads, 0, s>>>(a, c);
+      else
+        distill_stream_kernel<DT, false><<<kSms * kStreamCtas, kStreamThreads, 0, s>>>(a, c);
+      return cudaGetLastError();
+    default:
+      return h.n == 4 ? launch_team<DT, 4>(a, c, 1, s) : launch_team<DT, kWarps>(a, c, h.split, s);
   }
-  const int64_t bytes = (int64_t)V * (int64_t)sizeof(elem_t<DT>);
-  // CTAs that stay where rows are long enough for one warp to keep up with their lists, and leave few of them without a
-  // row at the end (4096 x 128000 179 us -> 162, 2048 x 50001 45 -> 39, 4096 x 32000 fp16 with tail 66 -> 54).
-  constexpr int64_t kCtas = 152 * kStreamCtas;
-  const int64_t turns = (a.rows + kCtas - 1) / kCtas;
-  if (bytes >= 32768 && V <= kStreamVocab && a.rows >= kCtas * 2 && a.rows * 100 >= turns * kCtas * 85) {
-    if (a.tail)
-      distill_stream_kernel<DT, true><<<(unsigned int)kCtas, kStreamThreads, 0, s>>>(a, c);
-    else
-      distill_stream_kernel<DT, false><<<(unsigned int)kCtas, kStreamThreads, 0, s>>>(a, c);
-    return cudaGetLastError();
-  }
-  // Else four warps for a row, however many rows there are (4096 x 128000 bf16 329 us with one, 205 with two, 179 with
-  // four, 189 with eight; 2048 x 50001 74, 49, 45, 50; 4096 x 32000 fp16 with tail 106, 79, 66, 92; 4000 x 16380 bf16, not
-  // long enough for the above, 37 with two, 29 with four), or eight where all rows run at once with these.
-  if (a.rows * kWarps > 32 * 152) return launch_team<DT, 4>(a, c, 1, s);
-  int split = 1;
-  while (split < kMaxCluster && a.rows * split * 2 <= 152 && V / (split * 2) >= 2048) split *= 2;
-  return launch_team<DT, kWarps>(a, c, split, s);
 }
 
 template <int DT, int P>
@@ -1384,10 +1364,9 @@ cudaError_t launch_backward_small(const mca_distill_backward_args& a, bool same,
 
 template <int DT>
 cudaError_t launch_backward_t(const mca_distill_backward_args& a, cudaStream_t s) {
-  const int V = a.vocab;
   const bool same = (reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.grad)) % 16 == 0 &&
                     (a.rows == 1 || (a.ld - a.ldg) % Pieces<DT>::N == 0);
-  const int64_t count = pieces_of<DT>(V);
+  const int64_t count = most_pieces(a.vocab, Pieces<DT>::N);
   if (count <= 32) return launch_backward_small<DT, 1>(a, same, s);
   if (count <= 64) return launch_backward_small<DT, 2>(a, same, s);
   if (count <= 128) return launch_backward_small<DT, 4>(a, same, s);

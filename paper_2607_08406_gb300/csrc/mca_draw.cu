@@ -19,6 +19,7 @@
 #include "mca_answers.h"
 #include "mca_device.cuh"
 #include "mca_elem.cuh"
+#include "mca_row_shapes.h"
 #include "mca_rows.cuh"
 
 namespace mca {
@@ -26,11 +27,9 @@ namespace mca {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kThreads = 256;
-constexpr int kCtas = 3;                   // per SM: 80 registers a thread, with which constants stay there (with 64 and
+constexpr int kWarps = kTeamWarps, kThreads = 32 * kWarps;
+constexpr int kCtas = kDrawCtas;           // per SM: 80 registers a thread, with which constants stay there (with 64 and
                                            // 32 warps 5000 x 50001 bf16 took 390 us, now 322)
-constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
 constexpr int kGroups = 8;                 // parts of a warp's pieces whose sums are kept
 constexpr int kFetch = 256;                // pieces (4 kB) that a warp asks for at once, to L2
 constexpr int kCopies = 8;                 // of the table, a quarter of the banks each (16 are no faster)
@@ -887,27 +886,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) verify_kernel(mca_verify_draf
     draw_last<DT, W, ROUND, true>(a, q, d, s, split, rank);
 }
 
-// Warps per row: few, so that what a row takes beside its logits is not a warp's all, but as many as run at once (6000 x
-// 10000 bf16: 147 us with sixteen, 74 with one). A CTA's warps at least where rows are few, or a cluster's CTAs. Rows of a
-// round have a kernel of their own, which draws from the steps that it has added up (16384 x 65 bf16 28 us in the others,
-// 15 here).
-struct Shape {
-  int warps = 1, split = 1;
-  bool round;                                // a row has 32 pieces at most, wherever it starts
-  Shape(int64_t rows, int64_t vocab, int n) : round((vocab + 2 * n - 2) / n <= 32) {
-    const int64_t pieces = vocab / n;
-    constexpr int64_t kAtOnce = kCtas * kWarps * 152, kRounds = 8;
-    while (warps < kWarps && (rows * warps < kAtOnce && pieces >= 64 * warps || pieces >= 32 * 32 * kRounds * warps))
-      warps *= 2;
-    if (warps == kWarps)
-      while (split < kMaxCluster && rows * split * 2 <= kCtas * 152 && pieces / (split * 2) >= 256) split *= 2;
-  }
-  int64_t grid(int64_t rows) const { return (rows * warps * split + kWarps - 1) / kWarps; }
-};
-
 // f(the shape's warps, and whether a row is a round, as types) with the launch that it says.
 template <class F>
-cudaError_t with_warps(const Shape& h, F f) {
+cudaError_t with_warps(const DrawShape& h, F f) {
   if (h.round) return f(std::integral_constant<int, 1>(), std::true_type());
   switch (h.warps) {
     case 1: return f(std::integral_constant<int, 1>(), std::false_type());
@@ -919,7 +900,7 @@ cudaError_t with_warps(const Shape& h, F f) {
 
 template <int DT>
 cudaError_t launch_sample(const mca_sample_tokens_args& a, cudaStream_t s) {
-  const Shape h(a.rows, a.vocab, Pieces<DT>::N);
+  const DrawShape h(a.rows, a.vocab, Pieces<DT>::N);
   return with_warps(h, [&](auto w, auto round) {
     return launch_clusters(sample_kernel<DT, decltype(w)::value, decltype(round)::value>, h.grid(a.rows), kThreads,
                            h.split, s, a, h.split);
@@ -928,7 +909,7 @@ cudaError_t launch_sample(const mca_sample_tokens_args& a, cudaStream_t s) {
 
 template <int DT>
 cudaError_t launch_verify(const mca_verify_drafts_args& a, cudaStream_t s) {
-  const Shape h(a.seqs, a.vocab, Pieces<DT>::N);
+  const DrawShape h(a.seqs, a.vocab, Pieces<DT>::N);
   return with_warps(h, [&](auto w, auto round) {
     return launch_clusters(verify_kernel<DT, decltype(w)::value, decltype(round)::value>, h.grid(a.seqs), kThreads,
                            h.split, s, a, h.split);
