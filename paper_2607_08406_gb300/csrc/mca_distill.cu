@@ -1132,6 +1132,7 @@ __global__ void __launch_bounds__(kSmallThreads) distill_backward_small_kernel(m
   Coefficients w;
   w.set(a, r, t);
   t.merge(a.top, a.vocab, s_seen[threadIdx.x / 32]);
+  __syncwarp();                                         // (the listed symbols' logits are read before another lane writes)
   if constexpr (P > 0) {
 #pragma unroll
     for (int i = 0; i < P; ++i)
@@ -1148,7 +1149,7 @@ __global__ void __launch_bounds__(kSmallThreads) distill_backward_small_kernel(m
       }
     }
   }
-  __syncwarp();                                         // (the listed symbols' logits are read, the others written)
+  __syncwarp();                                         // (the other symbols are written)
   write_listed<DT>(g.out, t, a.top, w, x, 0, a.vocab);
 }
 

@@ -260,3 +260,20 @@ def test_rows_in_turn_captured(gpu_lib, rows, vocab):
         for mine, ref in ((got, want[k]), (eager, want[1 - k])):
             for p, q in zip(mine, ref):
                 assert all(a is None or torch.equal(a, b) for a, b in zip(p, q))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("rows,vocab", [(3000, 300), (3000, 1001), (700, 4001), (930, 20003), (5, 100001)])
+def test_gradient_in_place_of_many_rows(gpu_lib, dtype, rows, vocab):
+    """Over the logits themselves, a hundred listed symbols in every part of the row: what it is beside them, bit for bit."""
+    import torch
+    x, index, t = case(vocab, rows, vocab, dtype, 100, 3, 1)
+    for tail in (False, True):
+        y = torch.empty(rows, vocab + 3, dtype=x.dtype, device="cuda")[:, :vocab]
+        y.copy_(x)
+        r = gpu_lib.mca_distill(y, index, t, tail=tail)
+        g = torch.linspace(-1.0, 2.0, rows, device="cuda")
+        out = torch.empty_strided(y.shape, y.stride(), dtype=y.dtype, device="cuda")
+        want = gpu_lib.mca_distill_backward(y, index, t, r.lse, g, rest=r.rest, out=out).clone()
+        assert gpu_lib.mca_distill_backward(y, index, t, r.lse, g, rest=r.rest, out=y) is y
+        assert torch.equal(y, want)
