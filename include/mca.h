@@ -558,10 +558,13 @@ mca_status mca_distill_backward(const mca_distill_backward_args* a);
 
 /* A symbol drawn from each row of logits with a given random number: token[r] = the first v of positive weight with
  * sum_{i <= v} w_i > u[r] * sum_i w_i, w_i = exp(logits[r, i]); u[r] in [0, 1) (below 0 as 0; from 1 on the last
- * symbol of positive weight). Cumulative sums are exact to 2^-32 of all weights and better (held in 64 bits
- * for u below 2^-24), so that the symbol is the definition's unless u lies that near to a border between two.
- * Temperatures, masks (-inf) and the like are the logits' own. Special rows: u NaN: token = -1, logprob = NaN; every logit -inf: token = -1, logprob = lse = -inf;
- * a NaN or +inf among the logits: token = -1, logprob and lse NaN. */
+ * symbol of positive weight). The symbol is the definition's unless u * sum w_i lies nearer to a border between two than
+ * 2^-32 of all weights and vocab * 2^-40 of the largest: weights are evaluated to 2^-33 of themselves and summed
+ * in steps of 2^-41.5 of the largest or less, of which a sum may be off by one for each symbol. (For u below 2^-24,
+ * logits beyond 1024 and more than 2^19 symbols they are summed in fp64.) lse and logprob come from such sums, rounded
+ * once. Temperatures, masks (-inf) and the like are the logits' own. Special rows: u NaN: token = -1, logprob = NaN;
+ * every logit -inf: token = -1, logprob = lse = -inf; a NaN or +inf among the logits: token = -1, logprob and lse
+ * NaN. Any other row has a token. */
 typedef struct {
   const void* logits;      /* [rows x vocab] of `dtype` */
   int32_t dtype;           /* mca_dtype */
@@ -583,8 +586,9 @@ mca_status mca_sample_tokens(const mca_sample_tokens_args* a);
  * where symbol a is the first that is not from the weights max(p_a(v) - q_a(v), 0), or p_a if these are all 0.
  * out[s, :]: the symbols kept, the one drawn, then -1; accepted[s]: how many were kept; logprob[s, :]: ln p_i of
  * what out holds, 0 behind it. Of each sequence one row of each net is read, beside the drafted symbols' logits. The
- * log-sum-exps are those of mca_token_logprobs. Probabilities are exact to 2^-32, so that sums of max(p - q, 0) are
- * to 2^-32 of those of p + q (where they come to less than 2^-10 they are held in 64 bits).
+ * log-sum-exps are those of mca_token_logprobs. Probabilities are evaluated to 2^-32 of themselves and summed in steps of
+ * 2^-43, so that the symbol drawn is the definition's unless u times the sum lies nearer to a border than 2^-32 of the
+ * sums of p and q and vocab * 2^-42 (sums that come to less than 2^-10 are held in fp64).
  * Special: lengths[s] outside 0..drafts: accepted = -1, out = -1, logprob NaN. A drafted symbol outside the
  * vocabulary, or a NaN in a decision: the sequence ends before it, with -1 and logprob NaN in its place; likewise
  * where a draw finds no symbol (no weight, a NaN or an infinity among weights, u NaN). */

@@ -3,8 +3,10 @@
 //
 // A drawn symbol is where the cumulative sum of weights passes u times their sum, and every weight before it moves its
 // border: with sums in fp32 one row in twenty of 128000 symbols would give a neighbour. So weights have an error of 2^-33 of
-// themselves at most (2^-32 where a log-sum-exp is taken off), and are summed as integers, in steps of 2^-43: a weight is
-// the same number of steps in every sum, whatever the order.
+// themselves at most (2^-32 where a log-sum-exp is taken off), and are summed as integers, in steps of 2^-43 of a power of
+// two that is at most 2^1.5 times the largest weight: a weight is the same number of steps in every sum, whatever the order.
+// Each symbol may be off by half a step, with one sign for many that are equal, and a lane by two where a larger logit
+// makes the steps coarser, which its four symbols and more share: by a step a symbol in all.
 //
 // x = n ln2 / 128 + d + e: an integer n, ln2 / 128 in two parts, so that d is exact, and e is what the second part gives.
 // 2^(n / 128) is a power of two times one of 128 numbers T in a table, each with the logarithm of what its rounding left
