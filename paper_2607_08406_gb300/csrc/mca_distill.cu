@@ -256,7 +256,7 @@ __device__ __forceinline__ uint4 without(const uint4& q, unsigned int bits) {
 
 // ------------------------------------------------------------------------------------------------
 // Short rows: a warp for each, P pieces to a lane, all in registers. A row is bound by the instructions around its list
-// (60000 x 300 bf16 against 32 symbols: 130 us with a warp and a ring of pieces for each, here 35, and 43 with tail).
+// (60000 x 300 bf16 against 32 symbols: 130 us with a warp and a ring of pieces for each, here 37, and 44 with tail).
 // ------------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 128;
 
